@@ -320,7 +320,7 @@ def run(s):
         return [s["dX"], s["dW"]] + [t for t in (s["dbias"], s["dmul"]) if t is not None]
     if case["op"] == "route":
         dass.expert_sort(s["ids"], case["E"], s["offsets"], s["order"], s["place"], workspace=s["workspace"])
-        dass.expert_gather(s["X"], s["order"], s["rows_out"])
+        dass.expert_gather(s["X"], s["place"], s["rows_out"])
         dass.expert_combine(s["Y"], s["place"], s["out"], weights=s["weights"], residual=s["residual"])
         return [s["offsets"], s["order"], s["place"], s["rows_out"], s["out"]]
     dass.expert_combine_backward(s["dout"], s["Y"], s["place"], s["weights"], s["rows_out"], s["dweights"])
