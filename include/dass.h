@@ -62,7 +62,8 @@ typedef DASS_ENUM(dass_act) {
     DASS_ACT_SILU = 0,
     DASS_ACT_GELU_TANH = 1,
     DASS_ACT_GELU_ERF = 2,
-    DASS_ACT_RELU = 3
+    DASS_ACT_RELU = 3,
+    DASS_ACT_NONE = 4       /* dass_linear and its gradient only */
 } dass_act;
 
 /* A dimension of a row-major matrix W[rows, cols]. */
@@ -342,6 +343,150 @@ dass_status dass_down_proj_sparse24(const void *Y, int64_t T, int64_t ldy, const
                                     int64_t ldv, const uint8_t *meta, int64_t ldm, int64_t d,
                                     int64_t d_int, dass_dtype dt, void *out, int64_t ldo,
                                     void *hip_stream);
+
+/*
+ * A mixture of GLU experts.  The MLP of Sec. 2.2 also occurs as a set of
+ * experts of which a router gives every token k: the pair (t, j) is token t's
+ * j-th choice.  The calls below bring the rows of an expert together, so that
+ * everything in this header that works on the rows of one MLP works on those
+ * of one expert, and take the experts' outputs back to the tokens.
+ *
+ * dass_expert_sort numbers the pairs by expert, stably:
+ *   experts  [T, k] ids of expert_bytes = 4 (int32) or 8 (int64) bytes, read
+ *            only.  An id outside 0 .. n_experts - 1 is a pair that goes nowhere
+ *            (a padded token, an expert of another device).  The same expert
+ *            twice for one token is two pairs.
+ *   offsets  [n_experts + 1] int32: expert e has the sorted rows
+ *            offsets[e] .. offsets[e + 1] - 1; offsets[n_experts] rows in all
+ *   order    [T k] int32: the pair t k + j of every sorted row, ascending within
+ *            an expert; -1 behind the last row
+ *   place    [T, k] int32: the sorted row of every pair; -1: it goes nowhere
+ *   n_experts 1 to 1024, k 1 to 64, T k below 2^31
+ *   workspace dass_expert_sort_workspace_bytes() bytes, 16-byte aligned (0
+ *            and NULL for few pairs).
+ * dass_expert_gather copies rows: out[place[t, j]] = X[t].  out has T k rows;
+ *   those that no pair has are left as they were.
+ * dass_expert_combine adds up: out[t] = residual[t] + sum_j weights[t, j] Y[place[t, j]],
+ *   in f32 in the order of the slots, residual first, rounded once.  weights
+ *   NULL: all 1, and without a residual that is the gradient of the gather.  A pair
+ *   that goes nowhere adds nothing; its row is not read.  residual may be NULL and may be out
+ *   itself.
+ * dass_expert_combine_backward: dY[place[t, j]] = weights[t, j] dout[t] and
+ *   dweights[t, j] = dout[t] . Y[place[t, j]] (f32; 0 for a pair that goes
+ *   nowhere); rows of dY that no pair has are left as they were.  The gradient of the
+ *   residual is dout.
+ *
+ * X, out of the gather etc. are rows of d elements of dtype dt; d is a multiple
+ * of 8 (bf16) or 4 (f32).  Entries of place outside 0 .. T k - 1 count as
+ * pairs that go nowhere.  place must not hold a row twice where rows are written.
+ */
+size_t dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t n_experts);
+
+dass_status dass_expert_sort(const void *experts, int expert_bytes, int64_t T, int64_t k,
+                             int64_t n_experts, int32_t *offsets, int32_t *order, int32_t *place,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+
+dass_status dass_expert_gather(const void *X, int64_t T, int64_t ldx, int64_t d, dass_dtype dt,
+                               const int32_t *place, int64_t k, void *out, int64_t ldo,
+                               void *hip_stream);
+
+dass_status dass_expert_combine(const void *Y, int64_t ldy, const int32_t *place, int64_t T,
+                                int64_t k, const float *weights, const void *residual, int64_t ldr,
+                                int64_t d, dass_dtype dt, void *out, int64_t ldo, void *hip_stream);
+
+dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const void *Y, int64_t ldy,
+                                         const int32_t *place, int64_t T, int64_t k,
+                                         const float *weights, int64_t d, dass_dtype dt, void *dY,
+                                         int64_t lddy, float *dweights, void *hip_stream);
+
+/*
+ * A linear layer with its epilogue, for all rows or by expert:
+ *
+ *   pre[t, i] = X[t, :] . W[e, i, :] + bias[e, i]
+ *   out[t, i] = act(pre[t, i]) * mul[t, i] + residual[t, i]
+ *
+ * e is 0, or with offsets the expert of row t: offsets[e] <= t < offsets[e + 1].
+ * Rows of no expert are left as they were.  offsets must not fall and stays
+ * within 0 .. T (a bound outside counts as the nearest one inside).  With mul the
+ * gate product of a GLU takes the up product along (Eq. 2): a GLU expert is three of these calls.
+ *
+ *   X        [T, d_in] row stride ldx;  W [d_out, d_in] row stride ldw, and
+ *            expert_stride elements from one expert's to the next's
+ *   offsets  NULL (n_experts = 1) or [n_experts + 1] int32, n_experts 1 to 1024
+ *   bias     NULL or [n_experts, d_out];  mul, residual NULL or [T, d_out]
+ *   pre_out  NULL or [T, d_out]: pre, as the gradient needs it
+ *   out      [T, d_out]; may be mul or residual itself (same stride), but no
+ *            other operand
+ * All of dtype dt (bf16 or f32); sums and epilogue are f32, rounded once (pre
+ * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32), T below 2^31.
+ *
+ * dass_linear_backward gives, with g = dout * mul * act'(pre),
+ *
+ *   dX[t, :] = sum_i g[t, i] W[e, i, :]          dbias[e, i] = sum over e's rows of g[t, i]
+ *   dW[e, i, :] = sum over e's rows of g[t, i] X[t, :]      dmul = dout * act(pre)
+ *
+ * each where its pointer is not NULL (the gradient of residual is dout).  An
+ * expert without rows gets zeros in dW and dbias; rows of no expert are left as
+ * they were in dX and dmul.  pre may be NULL if act is DASS_ACT_NONE and
+ * dmul is not asked for.  Outputs must not overlap inputs.  g is rounded to dt for the two products, and dbias
+ * is summed before that; everything else is f32 and rounded once.  Sums have a fixed order: the same
+ * bits on every run.
+ *   workspace  dass_linear_backward_workspace_bytes() bytes, 16-byte aligned (g
+ *            and partial sums)
+ */
+typedef struct {
+    const void *X;
+    int64_t T, ldx;
+    const void *W;
+    int64_t ldw, expert_stride;
+    int64_t d_in, d_out;
+    const int32_t *offsets;
+    int64_t n_experts;
+    const void *bias;
+    const void *mul;
+    int64_t ldm;
+    const void *residual;
+    int64_t ldr;
+    void *pre_out;
+    int64_t ldp;
+    void *out;
+    int64_t ldo;
+    dass_dtype dt;
+    dass_act act;
+} dass_linear_task;
+
+dass_status dass_linear(const dass_linear_task *task, void *hip_stream);
+
+typedef struct {
+    const void *dout;
+    int64_t T, ldg;
+    const void *X;
+    int64_t ldx;
+    const void *W;
+    int64_t ldw, expert_stride;
+    int64_t d_in, d_out;
+    const int32_t *offsets;
+    int64_t n_experts;
+    const void *pre;
+    int64_t ldp;
+    const void *mul;
+    int64_t ldm;
+    void *dX;
+    int64_t lddx;
+    void *dW;
+    int64_t lddw, dw_stride;
+    void *dbias;
+    void *dmul;
+    int64_t lddm;
+    dass_dtype dt;
+    dass_act act;
+} dass_linear_grad_task;
+
+size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt,
+                                            int64_t n_experts);
+
+dass_status dass_linear_backward(const dass_linear_grad_task *task, void *workspace,
+                                 size_t workspace_bytes, void *hip_stream);
 
 /* Name of a status code; never NULL. */
 const char *dass_status_string(dass_status s);

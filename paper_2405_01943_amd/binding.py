@@ -19,6 +19,7 @@ _LIB_PATH = os.path.join(_HERE, "libdass.so")
 _F32 = torch.float32
 DTYPE = {torch.float32: 0, torch.bfloat16: 1}
 ACT = {"silu": 0, "gelu_tanh": 1, "gelu_erf": 2, "relu": 3}
+LINEAR_ACT = {**ACT, "none": 4}      # of linear and its gradient
 AXIS = {"rows": 0, "cols": 1}
 
 EXPORTS = (
@@ -28,6 +29,9 @@ EXPORTS = (
     "dass_unstructured_workspace_bytes", "dass_score_mask_unstructured", "dass_score_mask_unstructured_static",
     "dass_input_norms_workspace_bytes", "dass_input_norms",
     "dass_mlp_forward_workspace_bytes", "dass_mlp_forward", "dass_compress_24", "dass_down_proj_sparse24",
+    "dass_expert_sort_workspace_bytes", "dass_expert_sort", "dass_expert_gather", "dass_expert_combine",
+    "dass_expert_combine_backward",
+    "dass_linear", "dass_linear_backward_workspace_bytes", "dass_linear_backward",
     "dass_status_string", "dass_last_error_string", "dass_version",
 )
 
@@ -37,6 +41,31 @@ class NmTask(ctypes.Structure):
     _fields_ = [("W", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("ld", ctypes.c_int64), ("norms", ctypes.c_void_p), ("norm_axis", ctypes.c_int),
                 ("group_axis", ctypes.c_int), ("alpha", ctypes.c_double), ("mask_out", ctypes.c_void_p)]
+
+
+class LinearTask(ctypes.Structure):
+    """dass_linear_task of include/dass.h."""
+    _fields_ = [("X", ctypes.c_void_p), ("T", ctypes.c_int64), ("ldx", ctypes.c_int64),
+                ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64), ("expert_stride", ctypes.c_int64),
+                ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64),
+                ("offsets", ctypes.c_void_p), ("n_experts", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("mul", ctypes.c_void_p), ("ldm", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("pre_out", ctypes.c_void_p), ("ldp", ctypes.c_int64), ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64),
+                ("dt", ctypes.c_int), ("act", ctypes.c_int)]
+
+
+class LinearGradTask(ctypes.Structure):
+    """dass_linear_grad_task of include/dass.h."""
+    _fields_ = [("dout", ctypes.c_void_p), ("T", ctypes.c_int64), ("ldg", ctypes.c_int64),
+                ("X", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64), ("expert_stride", ctypes.c_int64),
+                ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64),
+                ("offsets", ctypes.c_void_p), ("n_experts", ctypes.c_int64),
+                ("pre", ctypes.c_void_p), ("ldp", ctypes.c_int64), ("mul", ctypes.c_void_p), ("ldm", ctypes.c_int64),
+                ("dX", ctypes.c_void_p), ("lddx", ctypes.c_int64),
+                ("dW", ctypes.c_void_p), ("lddw", ctypes.c_int64), ("dw_stride", ctypes.c_int64),
+                ("dbias", ctypes.c_void_p), ("dmul", ctypes.c_void_p), ("lddm", ctypes.c_int64),
+                ("dt", ctypes.c_int), ("act", ctypes.c_int)]
 
 
 class DassError(RuntimeError):
@@ -102,6 +131,22 @@ def load_library() -> ctypes.CDLL:
     lib.dass_compress_24.argtypes = [vp, i64, i64, i64, ci, ci, vp, i64, vp, i64, vp, vp]
     lib.dass_down_proj_sparse24.restype = ci
     lib.dass_down_proj_sparse24.argtypes = [vp, i64, i64, vp, i64, vp, i64, i64, i64, ci, vp, i64, vp]
+    lib.dass_expert_sort_workspace_bytes.restype = sz
+    lib.dass_expert_sort_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.dass_expert_sort.restype = ci
+    lib.dass_expert_sort.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.dass_expert_gather.restype = ci
+    lib.dass_expert_gather.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, i64, vp]
+    lib.dass_expert_combine.restype = ci
+    lib.dass_expert_combine.argtypes = [vp, i64, vp, i64, i64, vp, vp, i64, i64, ci, vp, i64, vp]
+    lib.dass_expert_combine_backward.restype = ci
+    lib.dass_expert_combine_backward.argtypes = [vp, i64, vp, i64, vp, i64, i64, vp, i64, ci, vp, i64, vp, vp]
+    lib.dass_linear.restype = ci
+    lib.dass_linear.argtypes = [ctypes.POINTER(LinearTask), vp]
+    lib.dass_linear_backward_workspace_bytes.restype = sz
+    lib.dass_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, ci, i64]
+    lib.dass_linear_backward.restype = ci
+    lib.dass_linear_backward.argtypes = [ctypes.POINTER(LinearGradTask), vp, sz, vp]
     lib.dass_status_string.restype = ctypes.c_char_p
     lib.dass_status_string.argtypes = [ci]
     lib.dass_last_error_string.restype = ctypes.c_char_p
@@ -426,3 +471,218 @@ def down_proj_sparse24(Y: torch.Tensor, values: torch.Tensor, meta: torch.Tensor
     if status:
         _check(status)
 
+
+
+# ------------------------------------------------- a mixture of GLU experts --
+_I32 = torch.int32
+
+
+def _on_device(stream, *tensors) -> None:
+    """Every tensor of a call is on the GPU whose stream it is enqueued on."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        where = t.get_device()
+        if where < 0:
+            raise ValueError("every tensor must be on the GPU")
+        if device is None:
+            device = torch.cuda.current_device() if stream is None else stream.device_index
+        if where != device:
+            raise ValueError(f"a tensor on GPU {where}, the stream of GPU {device}")
+
+
+def _integers(t: torch.Tensor, name: str, shape) -> None:
+    if t.dtype != _I32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise TypeError(f"{name}: need contiguous int32 {tuple(shape)}")
+
+
+def expert_sort_workspace_bytes(T: int, k: int, n_experts: int) -> int:
+    return int(load_library().dass_expert_sort_workspace_bytes(T, k, n_experts))
+
+
+def expert_sort(experts: torch.Tensor, n_experts: int, offsets: torch.Tensor, order: torch.Tensor, place: torch.Tensor,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dass_expert_sort: the pairs of experts[T, k] (int32 or int64) numbered by expert.
+
+    offsets int32[n_experts + 1], order int32[T * k], place int32[T, k].
+    """
+    lib = load_library()
+    if experts.dtype not in (_I32, torch.int64) or experts.dim() != 2 or not experts.is_contiguous():
+        raise TypeError("experts: need contiguous int32 or int64 [T, k]")
+    T, k = experts.shape
+    _integers(offsets, "offsets", (n_experts + 1,))
+    _integers(order, "order", (T * k,))
+    _integers(place, "place", (T, k))
+    _on_device(stream, experts, offsets, order, place, workspace)
+    if workspace is None:
+        need = int(lib.dass_expert_sort_workspace_bytes(T, k, n_experts))
+        if need > 0:
+            workspace = _scratch(need, experts.device, stream)
+    status = lib.dass_expert_sort(_ptr(experts), experts.element_size(), T, k, n_experts, _ptr(offsets), _ptr(order),
+                                  _ptr(place), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if status:
+        _check(status)
+
+
+def _rows_of_pairs(t: torch.Tensor, name: str, pairs: int, d: int, dtype) -> int:
+    rows, width, ld = _matrix(t, name)
+    if (rows, width) != (pairs, d) or t.dtype != dtype:
+        raise ValueError(f"{name}: need [{pairs}, {d}] in the dtype of the other rows")
+    return ld
+
+
+def expert_gather(X: torch.Tensor, place: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """dass_expert_gather: out[place[t, j]] = X[t]; place int32[T, k], out [T * k, d]."""
+    lib = load_library()
+    T, d, ldx = _matrix(X, "X")
+    k = place.shape[-1]
+    _integers(place, "place", (T, k))
+    ldo = _rows_of_pairs(out, "out", T * k, d, X.dtype)
+    _on_device(stream, X, place, out)
+    status = lib.dass_expert_gather(_ptr(X), T, ldx, d, DTYPE[X.dtype], _ptr(place), k, _ptr(out), ldo, _stream(stream))
+    if status:
+        _check(status)
+
+
+def expert_combine(Y: torch.Tensor, place: torch.Tensor, out: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dass_expert_combine: out[t] = residual[t] + sum_j weights[t, j] Y[place[t, j]].
+
+    Without weights and residual this is the gradient of expert_gather.
+    """
+    lib = load_library()
+    T, d, ldo = _matrix(out, "out")
+    k = place.shape[-1]
+    _integers(place, "place", (T, k))
+    ldy = _rows_of_pairs(Y, "Y", T * k, d, out.dtype)
+    ldr = 0 if residual is None else _rows_of_pairs(residual, "residual", T, d, out.dtype)
+    if weights is not None and (weights.dtype != _F32 or weights.shape != place.shape or not weights.is_contiguous()):
+        raise TypeError("weights: need contiguous float32 [T, k]")
+    _on_device(stream, Y, place, out, weights, residual)
+    status = lib.dass_expert_combine(_ptr(Y), ldy, _ptr(place), T, k, _ptr(weights), _ptr(residual), ldr, d, DTYPE[out.dtype],
+                                     _ptr(out), ldo, _stream(stream))
+    if status:
+        _check(status)
+
+
+def expert_combine_backward(dout: torch.Tensor, Y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, dY: torch.Tensor,
+                            dweights: torch.Tensor, stream=None) -> None:
+    """dass_expert_combine_backward: dY[place[t, j]] = weights[t, j] dout[t], dweights[t, j] = dout[t] . Y[place[t, j]]."""
+    lib = load_library()
+    T, d, ldg = _matrix(dout, "dout")
+    k = place.shape[-1]
+    _integers(place, "place", (T, k))
+    ldy = _rows_of_pairs(Y, "Y", T * k, d, dout.dtype)
+    lddy = _rows_of_pairs(dY, "dY", T * k, d, dout.dtype)
+    for name, t in (("weights", weights), ("dweights", dweights)):
+        if t.dtype != _F32 or t.shape != place.shape or not t.is_contiguous():
+            raise TypeError(f"{name}: need contiguous float32 [T, k]")
+    _on_device(stream, dout, Y, place, weights, dY, dweights)
+    status = lib.dass_expert_combine_backward(_ptr(dout), ldg, _ptr(Y), ldy, _ptr(place), T, k, _ptr(weights), d,
+                                              DTYPE[dout.dtype], _ptr(dY), lddy, _ptr(dweights), _stream(stream))
+    if status:
+        _check(status)
+
+
+def _weights(W: torch.Tensor, name: str, n_experts: int, dtype):
+    """[d_out, d_in], or [n_experts, d_out, d_in] with offsets -> (d_out, d_in, row stride, expert stride)."""
+    stride = W.stride()
+    if len(stride) != (3 if n_experts else 2) or stride[-1] != 1 or W.dtype != dtype or (n_experts and W.shape[0] != n_experts):
+        raise TypeError(f"{name}: need {f'[{n_experts}, d_out, d_in]' if n_experts else '[d_out, d_in]'} with unit column "
+                        "stride in the dtype of X")
+    d_out, d_in = W.shape[-2:]
+    ld = stride[-2] if d_out > 1 else max(stride[-2], d_in)
+    return d_out, d_in, ld, stride[0] if n_experts > 1 else d_out * ld
+
+
+def _like(t: Optional[torch.Tensor], name: str, shape, dtype) -> int:
+    """The row stride of an optional matrix of the given shape."""
+    if t is None:
+        return 0
+    rows, cols, ld = _matrix(t, name)
+    if (rows, cols) != shape or t.dtype != dtype:
+        raise ValueError(f"{name}: need [{shape[0]}, {shape[1]}] in the dtype of X")
+    return ld
+
+
+def _expert_count(offsets: Optional[torch.Tensor]) -> int:
+    """0 without offsets."""
+    if offsets is None:
+        return 0
+    if offsets.dtype != _I32 or offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+        raise TypeError("offsets: need contiguous int32 [n_experts + 1]")
+    return offsets.numel() - 1
+
+
+def _bias(t: Optional[torch.Tensor], name: str, n_experts: int, d_out: int, dtype) -> None:
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != ((n_experts, d_out) if n_experts else (d_out,))
+                          or not t.is_contiguous()):
+        raise TypeError(f"{name}: need contiguous {'[n_experts, d_out]' if n_experts else '[d_out]'} in the dtype of X")
+
+
+def linear(X: torch.Tensor, W: torch.Tensor, out: torch.Tensor, act: str = "none", bias: Optional[torch.Tensor] = None,
+           mul: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+           pre_out: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dass_linear: out = act(X W^T + bias) * mul + residual.
+
+    Dense: W [d_out, d_in], bias [d_out].  By expert: offsets int32[n_experts + 1] (as expert_sort leaves
+    it), W [n_experts, d_out, d_in], bias [n_experts, d_out]; row t takes its expert's.  pre_out receives
+    X W^T + bias for the gradient.
+    """
+    lib = load_library()
+    T, d, ldx = _matrix(X, "X")
+    E, dt, code = _expert_count(offsets), X.dtype, LINEAR_ACT[act]
+    d_out, d_in, ldw, per_expert = _weights(W, "W", E, dt)
+    if d_in != d:
+        raise ValueError("W: rows must be as long as those of X")
+    shape = (T, d_out)
+    ldm, ldr = _like(mul, "mul", shape, dt), _like(residual, "residual", shape, dt)
+    ldp, ldo = _like(pre_out, "pre_out", shape, dt), _like(out, "out", shape, dt)
+    _bias(bias, "bias", E, d_out, dt)
+    _on_device(stream, X, W, out, bias, mul, residual, pre_out, offsets)
+    task = LinearTask(_ptr(X), T, ldx, _ptr(W), ldw, per_expert, d_in, d_out, _ptr(offsets), max(E, 1), _ptr(bias), _ptr(mul),
+                      ldm, _ptr(residual), ldr, _ptr(pre_out), ldp, _ptr(out), ldo, DTYPE[dt], code)
+    status = lib.dass_linear(ctypes.byref(task), _stream(stream))
+    if status:
+        _check(status)
+
+
+def linear_backward_workspace_bytes(T: int, d_in: int, d_out: int, dtype: torch.dtype, n_experts: int = 1) -> int:
+    return int(load_library().dass_linear_backward_workspace_bytes(T, d_in, d_out, DTYPE[dtype], n_experts))
+
+
+def linear_backward(dout: torch.Tensor, X: Optional[torch.Tensor], W: torch.Tensor, act: str = "none",
+                    pre: Optional[torch.Tensor] = None, mul: Optional[torch.Tensor] = None,
+                    dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None,
+                    dbias: Optional[torch.Tensor] = None, dmul: Optional[torch.Tensor] = None,
+                    offsets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dass_linear_backward: the gradients of linear that are given a tensor to go to.
+
+    pre is linear's pre_out (not needed for act "none" unless dmul is asked for), X is needed for dW alone.
+    """
+    lib = load_library()
+    T, d_out, ldg = _matrix(dout, "dout")
+    E, dt, code = _expert_count(offsets), dout.dtype, LINEAR_ACT[act]
+    do, d_in, ldw, per_expert = _weights(W, "W", E, dt)
+    if do != d_out:
+        raise ValueError("dout: rows must be as long as W has rows")
+    lddw = dw_per = 0
+    if dW is not None:
+        if tuple(dW.shape) != tuple(W.shape):
+            raise ValueError("dW: need the shape of W")
+        _, _, lddw, dw_per = _weights(dW, "dW", E, dt)
+    wide, narrow = (T, d_out), (T, d_in)
+    ldx, lddx = _like(X, "X", narrow, dt), _like(dX, "dX", narrow, dt)
+    ldp, ldm, lddm = _like(pre, "pre", wide, dt), _like(mul, "mul", wide, dt), _like(dmul, "dmul", wide, dt)
+    _bias(dbias, "dbias", E, d_out, dt)
+    _on_device(stream, dout, X, W, pre, mul, dX, dW, dbias, dmul, offsets, workspace)
+    if workspace is None:
+        need = int(lib.dass_linear_backward_workspace_bytes(T, d_in, d_out, DTYPE[dt], max(E, 1)))
+        workspace = _scratch(need, dout.device, stream)
+    task = LinearGradTask(_ptr(dout), T, ldg, _ptr(X), ldx, _ptr(W), ldw, per_expert, d_in, d_out, _ptr(offsets), max(E, 1),
+                          _ptr(pre), ldp, _ptr(mul), ldm, _ptr(dX), lddx, _ptr(dW), lddw, dw_per, _ptr(dbias), _ptr(dmul), lddm,
+                          DTYPE[dt], code)
+    status = lib.dass_linear_backward(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if status:
+        _check(status)

@@ -23,6 +23,7 @@
 //                      double-buffered; the K tail is masked.
 //
 // f32: calib_f32_kernel, the f32 matrix instruction on fragments straight from global memory.
+#include "activations.h"
 #include "dass_internal.h"
 #include "tile_order.h"
 
@@ -35,53 +36,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;  // one 16-byte chunk = 8 bf16
-
-// ------------------------------------------------------------- activations --
-template <int ACT>
-__device__ __forceinline__ float glu_act_fast(float g)
-{
-    // exp2 and the reciprocal are the hardware's 1-ulp instructions; a true division costs a
-    // dozen instructions per element and the bf16 path is good to 1e-6 without it.
-    if constexpr (ACT == DASS_ACT_SILU) {
-        return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g));
-    } else if constexpr (ACT == DASS_ACT_GELU_TANH) {
-        // 0.5 g (1 + tanh z) = g / (1 + exp(-2 z)),  z = sqrt(2/pi) (g + 0.044715 g^3)
-        // exp(-2 z) = exp2(g (c0 + c1 g^2)),  c0 = -2 sqrt(2/pi) log2(e),  c1 = 0.044715 c0
-        const float e = g * fmaf(-0.10294324f, g * g, -2.3022082f);
-        return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(e));
-    } else if constexpr (ACT == DASS_ACT_GELU_ERF) {
-        // erf by the classical five-term rational form in t = 1 / (1 + p z) times exp(-z^2)
-        // (Abramowitz & Stegun 7.1.26, absolute error of erf below 1.5e-7), written on z = |g| / sqrt(2)
-        // so that neither branch cancels: with h = (1 - erf z) / 2 = P(t) exp(-g^2 / 2) / 2,
-        // GELU(g) = g (1 - h) for g >= 0 and g h for g < 0.  The library's erff is several times the
-        // instructions; the norms are good to 1e-6 either way.
-        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.3275911f * 0.70710678f, 1.0f));
-        float P = fmaf(t, 1.061405429f, -1.453152027f);
-        P = fmaf(t, P, 1.421413741f);
-        P = fmaf(t, P, -0.284496736f);
-        P = fmaf(t, P, 0.254829592f);
-        const float h = 0.5f * t * P * __builtin_amdgcn_exp2f(g * g * -0.72134752f);   // exp(-g^2 / 2)
-        return g * (g >= 0.0f ? 1.0f - h : h);
-    } else {
-        return fmaxf(g, 0.0f);
-    }
-}
-
-__device__ __forceinline__ float glu_act_precise(float g, int act)
-{
-    switch (act) {
-    case DASS_ACT_SILU:
-        return g / (1.0f + expf(-g));
-    case DASS_ACT_GELU_TANH: {
-        const float z2 = 1.5957691216057308f * g * (1.0f + 0.044715f * g * g);
-        return g / (1.0f + expf(-z2));
-    }
-    case DASS_ACT_GELU_ERF:
-        return 0.5f * g * (1.0f + erff(g * 0.7071067811865476f));
-    default:
-        return fmaxf(g, 0.0f);
-    }
-}
 
 // ------------------------------------------------------- small helper kernels --
 __global__ void fill_zero_kernel(float *p, int64_t n)

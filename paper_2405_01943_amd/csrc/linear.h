@@ -1,0 +1,147 @@
+// What the kernels of dass_linear and dass_linear_backward share: rows that are grouped by expert, the epilogue, and the
+// launches behind the entry points.
+#pragma once
+
+#include "activations.h"
+#include "chunk.h"
+#include "dass_internal.h"
+
+namespace dass {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+// Rows [offsets[e], offsets[e + 1]) belong to expert e; offsets = nullptr: all rows to one.  The bounds are held to
+// [0, rows] whatever the array holds, so that no row outside the matrices is ever addressed.
+struct Segments {
+    const int32_t *offsets;
+    int64_t rows;
+    int n;
+};
+
+struct Span {
+    int64_t lo, hi;
+};
+
+__device__ __forceinline__ Span segment(const Segments &s, int e)
+{
+    if (!s.offsets)
+        return {0, s.rows};
+    const int64_t a = s.offsets[e], b = s.offsets[e + 1];
+    const int64_t lo = a < 0 ? 0 : a < s.rows ? a : s.rows, hi = b < lo ? lo : b < s.rows ? b : s.rows;
+    return {lo, hi};
+}
+
+// Tiles of `bm` rows that do not cross experts, numbered without a scan: expert e's first tile is number
+// floor(lo_e / bm) + e.  These numbers rise by more than an expert has tiles (ceil(n / bm) <= floor((lo + n) / bm) -
+// floor(lo / bm) + 1), so floor(rows / bm) + n numbers hold every tile, some of them none.  A wavefront finds the
+// expert of a number by counting the first tiles that are not beyond it, 64 experts at a time.
+__device__ __forceinline__ bool rows_of_tile(const Segments &s, int64_t number, int bm, int &expert, Span &span)
+{
+    expert = 0;
+    if (!s.offsets) {
+        span = {number * bm, s.rows};
+        return span.lo < s.rows;
+    }
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int e0 = 0; e0 < s.n; e0 += 64) {
+        const int e = e0 + lane;
+        int64_t lo = e < s.n ? s.offsets[e] : 0;
+        lo = lo < 0 ? 0 : lo < s.rows ? lo : s.rows;
+        n += __popcll(__ballot(e < s.n && lo / bm + e <= number));
+    }
+    if (n == 0)
+        return false;   // offsets that do not begin with 0
+    expert = __builtin_amdgcn_readfirstlane(n - 1);
+    span = segment(s, expert);
+    const int64_t nth = number - (span.lo / bm + expert);
+    span.lo += nth * bm;
+    return nth >= 0 && span.lo < span.hi;   // (offsets that fall have no tiles)
+}
+
+inline int64_t tile_numbers(const Segments &s, int64_t bm)
+{
+    return s.offsets ? s.rows / bm + s.n : (s.rows + bm - 1) / bm;
+}
+
+// out = act(sum + bias) * mul + residual, pre = sum + bias.  Absent parts are nullptr.  All strides in elements.
+template <typename T_>
+struct Epilogue {
+    T_ *out;
+    int64_t ldo;
+    const T_ *bias;        // [n_experts][cols]
+    const T_ *mul;
+    int64_t ldm;
+    const T_ *residual;
+    int64_t ldr;
+    T_ *pre;
+    int64_t ldp;
+    int64_t cols;
+    int act;
+};
+
+// Four neighbouring elements as f32 and back: 8 bytes of bf16, 16 of f32.
+__device__ __forceinline__ f32x4 load4(const uint16_t *p)
+{
+    const uint2 c = *reinterpret_cast<const uint2 *>(p);
+    return f32x4{__builtin_bit_cast(float, c.x << 16), __builtin_bit_cast(float, c.x & 0xffff0000u),
+                 __builtin_bit_cast(float, c.y << 16), __builtin_bit_cast(float, c.y & 0xffff0000u)};
+}
+__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+__device__ __forceinline__ void store4(uint16_t *p, const f32x4 &v)
+{
+    typedef __attribute__((ext_vector_type(2))) float f2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+    uint2 c;
+    c.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[0], v[1]}, b2));
+    c.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[2], v[3]}, b2));
+    *reinterpret_cast<uint2 *>(p) = c;
+}
+__device__ __forceinline__ void store4(float *p, const f32x4 &v) { *reinterpret_cast<f32x4 *>(p) = v; }
+
+// Four neighbouring columns of one row; `col` is a multiple of 4 and inside.
+template <typename T_>
+__device__ __forceinline__ void finish4(const Epilogue<T_> &ep, int expert, int64_t row, int64_t col, f32x4 v)
+{
+    constexpr bool FAST = sizeof(T_) == 2;
+    if (ep.bias)
+        v += load4(ep.bias + (int64_t)expert * ep.cols + col);
+    if (ep.pre)
+        store4(ep.pre + row * ep.ldp + col, v);
+    if (ep.act != DASS_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = act_value<FAST>(v[i], ep.act);
+    }
+    if (ep.mul)
+        v *= load4(ep.mul + row * ep.ldm + col);
+    if (ep.residual)
+        v += load4(ep.residual + row * ep.ldr + col);
+    store4(ep.out + row * ep.ldo + col, v);
+}
+
+// C[r, c] = sum over k of P[r, k] Q[c, k], r the rows of the output and c its contiguous columns.  An operand is stored
+// either row by row (k contiguous) or k by k (r or c contiguous); three of the four combinations occur:
+//   forward  P = X  [rows, d_in],  Q = W [d_out, d_in]            both by rows, r in the rows of an expert
+//   dX       P = g  [rows, d_out], Q = W [d_out, d_in]            Q k by k, r in the rows of an expert
+//   dW       P = g, Q = X                                         both k by k, k in the rows of an expert
+enum Product { kForward, kInputGrad, kWeightGrad };
+
+template <typename T_>
+struct Operands {
+    const T_ *P, *Q;
+    int64_t ldp, ldq;
+    int64_t q_stride;      // forward, dX: elements from one expert's Q to the next
+    int64_t out_stride;    // dW: elements from one expert's C to the next
+    int64_t out_rows;      // dW: rows of C
+    int64_t depth;         // forward, dX: k
+    Segments seg;
+};
+
+// One launch each; errors as the entry points report them.
+dass_status launch_product_f32(const char *fn, Product product, const Operands<float> &a, const Epilogue<float> &ep,
+                               hipStream_t stream);
+dass_status launch_product_bf16(const char *fn, Product product, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,
+                                hipStream_t stream);
+
+}  // namespace dass

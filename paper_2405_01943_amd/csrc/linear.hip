@@ -1,0 +1,358 @@
+// dass_linear: out = act(X W^T + b) * mul + residual, with one W for all rows or that of each row's expert, and its
+// gradients.  This file has the checks, the element-wise part of the gradient and the bias sums; the products are in
+// linear_bf16.hip and linear_f32.hip.
+//
+// Gradients, with g = dout * mul * act'(pre):  dX = g W,  dW = g^T X over an expert's rows,  db = sum of its g,
+// dmul = dout * act(pre).  g is read by both products, so it is written once, in dtype dt: rounded to bf16
+// there because the matrix cores take nothing wider (each term of a sum is off by half a step of its own, which adds about as
+// much to a sum as its own rounding does).  Without activation and mul, g is dout itself and nothing is written.
+#include "linear.h"
+
+namespace dass {
+
+constexpr int kMaxLinearExperts = 1024;
+
+// ------------------------------------------------------ element-wise gradient and sums --
+// A wavefront owns 64 chunks of 16 bytes of columns and every fourth row of a tile of rows of one expert.  One pass:
+// reads dout, pre and mul, writes g and dmul, and adds g up for the bias in f32 before it is rounded, over the tile.
+template <typename T_>
+__global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout, int64_t ldg, const T_ *__restrict__ pre,
+                                                    int64_t ldp, const T_ *__restrict__ mul, int64_t ldm, int act, int64_t cols,
+                                                    Segments seg, int tile_rows, T_ *__restrict__ g_out, T_ *__restrict__ dmul,
+                                                    int64_t lddm, float *__restrict__ partial, uint32_t strips)
+{
+    constexpr int N = Chunk<T_>::N;
+    constexpr bool FAST = sizeof(T_) == 2;
+    __shared__ float sums[4][64][N + 1];
+    const uint32_t number = blockIdx.x / strips, strip = blockIdx.x - number * strips;
+    int expert;
+    Span r;
+    if (!rows_of_tile(seg, number, tile_rows, expert, r))
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)strip * 64 + lane) * N;
+    const int64_t end = r.lo + tile_rows < r.hi ? r.lo + tile_rows : r.hi;
+    float sum[N];
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+        sum[x] = 0.0f;
+    if (c < cols) {
+        for (int64_t row = r.lo + wave; row < end; row += 4) {
+            float g[N], p[N], m[N];
+            Chunk<T_>::widen(*reinterpret_cast<const u32x4 *>(dout + row * ldg + c), g);
+            if (pre)
+                Chunk<T_>::widen(*reinterpret_cast<const u32x4 *>(pre + row * ldp + c), p);
+            if (mul)
+                Chunk<T_>::widen(*reinterpret_cast<const u32x4 *>(mul + row * ldm + c), m);
+            if (dmul) {
+                float y[N];
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    y[x] = g[x] * act_value<FAST>(p[x], act);
+                *reinterpret_cast<u32x4 *>(dmul + row * lddm + c) = Chunk<T_>::narrow(y);
+            }
+            if (mul) {
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    g[x] *= m[x];
+            }
+            if (act != DASS_ACT_NONE) {
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    g[x] *= act_slope<FAST>(p[x], act);
+            }
+            if (g_out)
+                *reinterpret_cast<u32x4 *>(g_out + row * cols + c) = Chunk<T_>::narrow(g);
+#pragma unroll
+            for (int x = 0; x < N; ++x)
+                sum[x] += g[x];
+        }
+    }
+    if (!partial)
+        return;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+        sums[wave][lane][x] = sum[x];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * N; i += 256) {
+        const int64_t col = (int64_t)strip * 64 * N + i;
+        if (col < cols) {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                s += sums[w][i / N][i % N];
+            partial[number * cols + col] = s;
+        }
+    }
+}
+
+// db[e] = sum of the partial sums of e's tiles, in a fixed order.  A workgroup owns 64 columns of one expert, its four
+// wavefronts every fourth tile.
+template <typename T_>
+__global__ __launch_bounds__(256) void bias_kernel(const float *__restrict__ partial, int64_t cols, Segments seg, int tile_rows,
+                                                   T_ *__restrict__ dbias)
+{
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, expert = blockIdx.y;
+    const Span r = segment(seg, expert);
+    const int64_t first = seg.offsets ? r.lo / tile_rows + expert : 0, tiles = (r.hi - r.lo + tile_rows - 1) / tile_rows;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (c < cols) {
+#pragma unroll 8
+        for (int64_t i = wave; i < tiles; i += 4)
+            s += partial[(first + i) * cols + c];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+        s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        if constexpr (sizeof(T_) == 2)
+            dbias[(int64_t)expert * cols + c] = __builtin_bit_cast(uint16_t, (__bf16)s);
+        else
+            dbias[(int64_t)expert * cols + c] = s;
+    }
+}
+
+// ------------------------------------------------------------------ host side --
+// Rows of a tile of the two kernels above: 64, more where that makes over 512 tiles, whose sums one workgroup adds.
+static int sum_tile_rows(int64_t rows)
+{
+    int64_t t = 64;
+    while (rows / t > 512)
+        t *= 2;
+    return (int)(t < (1 << 24) ? t : 1 << 24);
+}
+
+static size_t kept_bytes(int64_t rows, int64_t d_out, dass_dtype dt)
+{
+    return round_up((size_t)rows * (size_t)d_out * elem_bytes(dt), 256);
+}
+
+static size_t partial_bytes(int64_t rows, int64_t d_out, int64_t n_experts)
+{
+    return round_up((size_t)(rows / sum_tile_rows(rows) + 1 + n_experts) * (size_t)d_out * 4, 256);
+}
+
+struct Checker {
+    const char *fn;
+    int vec;
+    dass_status status = DASS_OK;
+
+    // a matrix of `rows` rows of `width` elements; absent optional ones are fine
+    void matrix(const char *name, const void *p, int64_t ld, int64_t width, bool required)
+    {
+        if (status != DASS_OK || (!p && !required))
+            return;
+        if (!p)
+            status = fail(DASS_ERR_NULL, "%s: %s must not be NULL", fn, name);
+        else if (ld < width)
+            status = fail(DASS_ERR_SHAPE, "%s: row stride %lld of %s is shorter than its rows of %lld", fn, (long long)ld, name,
+                          (long long)width);
+        else if (!aligned16(p) || ld % vec != 0)
+            status = fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
+    }
+    void vector(const char *name, const void *p)
+    {
+        if (status == DASS_OK && p && !aligned16(p))
+            status = fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned", fn, name);
+    }
+    void sizes(int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts, const int32_t *offsets, int dt, int act)
+    {
+        if (!valid_dtype(dt))
+            status = fail(DASS_ERR_DTYPE, "%s: unknown dtype %d", fn, dt);
+        else if (act < DASS_ACT_SILU || act > DASS_ACT_NONE)
+            status = fail(DASS_ERR_DTYPE, "%s: unknown activation %d", fn, act);
+        else if (T <= 0 || d_in <= 0 || d_out <= 0)
+            status = fail(DASS_ERR_SHAPE, "%s: T=%lld d_in=%lld d_out=%lld must be positive", fn, (long long)T, (long long)d_in,
+                          (long long)d_out);
+        else if (T > 0x7fffffffLL)
+            status = fail(DASS_ERR_SHAPE, "%s: T=%lld rows do not fit an int32", fn, (long long)T);
+        else if (d_in % vec_elems(dt) != 0 || d_out % vec_elems(dt) != 0)
+            status = fail(DASS_ERR_SHAPE, "%s: d_in=%lld and d_out=%lld must be multiples of %d", fn, (long long)d_in,
+                          (long long)d_out, vec_elems(dt));
+        else if (n_experts <= 0 || n_experts > kMaxLinearExperts || (!offsets && n_experts != 1))
+            status = fail(DASS_ERR_SHAPE, "%s: n_experts=%lld must be 1 without offsets, 1 to %d with them", fn,
+                          (long long)n_experts, kMaxLinearExperts);
+        else if (reinterpret_cast<uintptr_t>(offsets) & 3u)
+            status = fail(DASS_ERR_ALIGN, "%s: offsets must be 4-byte aligned", fn);
+    }
+    void stride(const char *name, int64_t stride, int64_t ld, int64_t d_in, int64_t d_out, int64_t n_experts)
+    {
+        if (status == DASS_OK && n_experts > 1 && stride < (d_out - 1) * ld + d_in)
+            status = fail(DASS_ERR_SHAPE, "%s: expert stride %lld of %s is shorter than a matrix", fn, (long long)stride, name);
+        if (status == DASS_OK && n_experts > 1 && stride % vec != 0)
+            status = fail(DASS_ERR_ALIGN, "%s: expert stride of %s must be a multiple of %d elements", fn, name, vec);
+    }
+};
+
+template <typename T_>
+static dass_status launch_product(const char *fn, Product product, const Operands<T_> &a, const Epilogue<T_> &ep, hipStream_t stream)
+{
+    if constexpr (sizeof(T_) == 2)
+        return launch_product_bf16(fn, product, a, ep, stream);
+    else
+        return launch_product_f32(fn, product, a, ep, stream);
+}
+
+template <typename T_>
+static dass_status run_linear(const char *fn, const dass_linear_task &t, hipStream_t stream)
+{
+    Operands<T_> a = {};
+    a.P = static_cast<const T_ *>(t.X);
+    a.ldp = t.ldx;
+    a.Q = static_cast<const T_ *>(t.W);
+    a.ldq = t.ldw;
+    a.q_stride = t.expert_stride;
+    a.depth = t.d_in;
+    a.seg = {t.offsets, t.T, (int)t.n_experts};
+    const Epilogue<T_> ep = {static_cast<T_ *>(t.out), t.ldo, static_cast<const T_ *>(t.bias), static_cast<const T_ *>(t.mul),
+                             t.ldm, static_cast<const T_ *>(t.residual), t.ldr, static_cast<T_ *>(t.pre_out), t.ldp, t.d_out,
+                             (int)t.act};
+    return launch_product(fn, kForward, a, ep, stream);
+}
+
+template <typename T_>
+static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &t, char *workspace, hipStream_t stream)
+{
+    constexpr int N = Chunk<T_>::N;
+    const Segments seg = {t.offsets, t.T, (int)t.n_experts};
+    const bool own_g = (t.act != DASS_ACT_NONE || t.mul) && (t.dX || t.dW);
+    const T_ *g = static_cast<const T_ *>(t.dout);
+    int64_t ldg = t.ldg;
+    if (own_g || t.dbias || t.dmul) {
+        T_ *kept = own_g ? reinterpret_cast<T_ *>(workspace) : nullptr;
+        float *partial = t.dbias ? reinterpret_cast<float *>(workspace + kept_bytes(t.T, t.d_out, t.dt)) : nullptr;
+        const int tile_rows = sum_tile_rows(t.T);
+        const int64_t numbers = tile_numbers(seg, tile_rows), strips = (t.d_out + 64 * N - 1) / (64 * N);
+        if (numbers > 0xffffffffLL / 256 / strips)
+            return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
+        hipLaunchKernelGGL(slope_kernel<T_>, dim3((unsigned)(numbers * strips)), dim3(256), 0, stream,
+                           static_cast<const T_ *>(t.dout), t.ldg, static_cast<const T_ *>(t.pre), t.ldp,
+                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, tile_rows, kept,
+                           static_cast<T_ *>(t.dmul), t.lddm, partial, (uint32_t)strips);
+        dass_status s = check_launch("slope kernel");
+        if (s != DASS_OK)
+            return s;
+        if (t.dbias) {
+            hipLaunchKernelGGL(bias_kernel<T_>, dim3((unsigned)((t.d_out + 63) / 64), (unsigned)t.n_experts), dim3(256), 0, stream,
+                               (const float *)partial, t.d_out, seg, tile_rows, static_cast<T_ *>(t.dbias));
+            s = check_launch("bias kernel");
+            if (s != DASS_OK)
+                return s;
+        }
+        if (own_g) {
+            g = kept;
+            ldg = t.d_out;
+        }
+    }
+    if (t.dX) {
+        Operands<T_> a = {};
+        a.P = g;
+        a.ldp = ldg;
+        a.Q = static_cast<const T_ *>(t.W);
+        a.ldq = t.ldw;
+        a.q_stride = t.expert_stride;
+        a.depth = t.d_out;
+        a.seg = seg;
+        Epilogue<T_> ep = {};
+        ep.out = static_cast<T_ *>(t.dX);
+        ep.ldo = t.lddx;
+        ep.cols = t.d_in;
+        ep.act = DASS_ACT_NONE;
+        const dass_status s = launch_product(fn, kInputGrad, a, ep, stream);
+        if (s != DASS_OK)
+            return s;
+    }
+    if (t.dW) {
+        Operands<T_> a = {};
+        a.P = g;
+        a.ldp = ldg;
+        a.Q = static_cast<const T_ *>(t.X);
+        a.ldq = t.ldx;
+        a.out_stride = t.dw_stride;
+        a.out_rows = t.d_out;
+        a.seg = seg;
+        Epilogue<T_> ep = {};
+        ep.out = static_cast<T_ *>(t.dW);
+        ep.ldo = t.lddw;
+        ep.cols = t.d_in;
+        ep.act = DASS_ACT_NONE;
+        return launch_product(fn, kWeightGrad, a, ep, stream);
+    }
+    return DASS_OK;
+}
+
+}  // namespace dass
+
+extern "C" dass_status dass_linear(const dass_linear_task *task, void *hip_stream)
+{
+    using namespace dass;
+    const char *fn = "dass_linear";
+    if (!task)
+        return fail(DASS_ERR_NULL, "%s: task must not be NULL", fn);
+    const dass_linear_task &t = *task;
+    Checker c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
+    c.sizes(t.T, t.d_in, t.d_out, t.n_experts, t.offsets, (int)t.dt, (int)t.act);
+    c.matrix("X", t.X, t.ldx, t.d_in, true);
+    c.matrix("W", t.W, t.ldw, t.d_in, true);
+    c.matrix("mul", t.mul, t.ldm, t.d_out, false);
+    c.matrix("residual", t.residual, t.ldr, t.d_out, false);
+    c.matrix("pre_out", t.pre_out, t.ldp, t.d_out, false);
+    c.matrix("out", t.out, t.ldo, t.d_out, true);
+    c.vector("bias", t.bias);
+    c.stride("W", t.expert_stride, t.ldw, t.d_in, t.d_out, t.n_experts);
+    if (c.status != DASS_OK)
+        return c.status;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    return t.dt == DASS_BF16 ? run_linear<uint16_t>(fn, t, stream) : run_linear<float>(fn, t, stream);
+}
+
+extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
+{
+    using namespace dass;
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt))
+        return 0;
+    return kept_bytes(T, d_out, dt) + partial_bytes(T, d_out, n_experts);
+}
+
+extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, void *workspace, size_t workspace_bytes,
+                                            void *hip_stream)
+{
+    using namespace dass;
+    const char *fn = "dass_linear_backward";
+    if (!task)
+        return fail(DASS_ERR_NULL, "%s: task must not be NULL", fn);
+    const dass_linear_grad_task &t = *task;
+    Checker c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
+    c.sizes(t.T, t.d_in, t.d_out, t.n_experts, t.offsets, (int)t.dt, (int)t.act);
+    if (c.status != DASS_OK)
+        return c.status;
+    if (!t.dX && !t.dW && !t.dbias && !t.dmul)
+        return fail(DASS_ERR_NULL, "%s: no gradient is asked for", fn);
+    if (t.dmul && !t.mul)
+        return fail(DASS_ERR_NULL, "%s: dmul without mul", fn);
+    c.matrix("dout", t.dout, t.ldg, t.d_out, true);
+    c.matrix("X", t.X, t.ldx, t.d_in, t.dW != nullptr);
+    c.matrix("W", t.W, t.ldw, t.d_in, t.dX != nullptr);
+    c.matrix("pre", t.pre, t.ldp, t.d_out, t.act != DASS_ACT_NONE || t.dmul);
+    c.matrix("mul", t.mul, t.ldm, t.d_out, false);
+    c.matrix("dX", t.dX, t.lddx, t.d_in, false);
+    c.matrix("dW", t.dW, t.lddw, t.d_in, false);
+    c.matrix("dmul", t.dmul, t.lddm, t.d_out, false);
+    c.vector("dbias", t.dbias);
+    if (t.dX)
+        c.stride("W", t.expert_stride, t.ldw, t.d_in, t.d_out, t.n_experts);
+    if (t.dW)
+        c.stride("dW", t.dw_stride, t.lddw, t.d_in, t.d_out, t.n_experts);
+    if (c.status != DASS_OK)
+        return c.status;
+    const size_t need = dass_linear_backward_workspace_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts);
+    if (!workspace || workspace_bytes < need)
+        return fail(DASS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
+    if (!aligned16(workspace))
+        return fail(DASS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", fn);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    char *ws = static_cast<char *>(workspace);
+    return t.dt == DASS_BF16 ? run_linear_grad<uint16_t>(fn, t, ws, stream) : run_linear_grad<float>(fn, t, ws, stream);
+}
