@@ -170,10 +170,4 @@ dass_status launch_product_f32(const char *fn, Product product, const Operands<f
     return launch_any(fn, product, a, ep, stream);
 }
 
-dass_status launch_product_bf16(const char *fn, Product product, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,
-                                hipStream_t stream)
-{
-    return launch_any(fn, product, a, ep, stream);
-}
-
 }  // namespace dass
