@@ -18,7 +18,7 @@
 // barrier of the slab, which stands where every wavefront has read its last fragments of it, in the middle of its second
 // K step; the loads of Q's slab s + NQ and P's slab s + NP are spread over the matrix instructions from there to the
 // next barrier.  The wait before a barrier counts the loads that may still be on their way, so their order is
-// pinned; only slabs that exist are requested, and the last NP slabs have bodies of their own with fewer to wait for.
+// pinned; only slabs that exist are requested, and the last slabs have bodies of their own with fewer to wait for.
 //
 // Reads outside a matrix: each operand is a raw buffer that starts at the tile's first row and ends with its last
 // valid element; what lies beyond reads as 0.  Lane offsets are 32-bit registers, the scalar offset is at most a row
@@ -55,22 +55,30 @@ __device__ __forceinline__ void for_each(F &&f)
 constexpr int kLds = 160 * 1024, kSlab = 64;
 constexpr int kOutside = 0x7fffffff;
 
-// One wave-load of 16 bytes a lane from a buffer straight into LDS.  By hand: beside the builtin the compiler waits for every such load
-// before each transposing LDS read (it takes the read to depend on them), which empties the pipeline once a
-// load.  The block writes no register but m0; the waits for it are those before the barriers.  The s_nop covers the wait
-// states between a scalar register's last write and its use as an address.
-__device__ __forceinline__ void load_to_lds(const u32x4 &buffer, char *dst, uint32_t lane_off, int off)
-{
-    const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr_t)dst;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(lane_off), "s"(buffer),
-                 "s"(off) : "m0", "memory");
-}
-
 // A raw buffer: 48 bits of address, no stride, its length in bytes.
 __device__ __forceinline__ u32x4 raw_buffer(const void *p, int bytes)
 {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
     return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+}
+
+// One wave-load of 16 bytes a lane from a buffer straight into LDS: the builtin where both operands are by rows, and
+// by hand where one is not.  Beside the builtin the compiler waits for every such load before each transposing LDS read (it takes the
+// read to depend on them), which empties the pipeline once a load: dX and dW of 6000 rows of 4096 x 11008 1590 us, by
+// hand 548 and 444; of products without such reads the builtin is 4 % ahead.  (Not a template: with arguments that depend on
+// one, the host pass rejects the builtin.)  The block by hand writes no register but m0; the waits for it are
+// those before the barriers.  Its s_nop covers the wait states between a scalar register's last write and its use as an address.
+__device__ __forceinline__ void load_to_lds(const u32x4 &buffer, char *dst, uint32_t lane_off, int off)
+{
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void *>((uint64_t)buffer[1] << 32 | buffer[0]), 0, (int)buffer[2], (int)buffer[3]);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, lane_off, off, 0, 0);
+}
+__device__ __forceinline__ void load_to_lds_by_hand(const u32x4 &buffer, char *dst, uint32_t lane_off, int off)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr_t)dst;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(lane_off), "s"(buffer),
+                 "s"(off) : "m0", "memory");
 }
 
 __device__ __forceinline__ void block_barrier()
@@ -89,11 +97,11 @@ __device__ __forceinline__ void wait_loads()
 }
 
 // One operand of a workgroup: its loads into LDS and its fragments from there.  B: blocks of 16 rows of a wavefront.
-template <bool BY_ROWS, int B>
+template <bool BY_ROWS, int B, bool BY_HAND>
 struct Part;
 
-template <int B>
-struct Part<true, B> {
+template <int B, bool BY_HAND>
+struct Part<true, B, BY_HAND> {
     static constexpr int LOADS = B, READS = B, UNIT = 32 * B * 128;
     struct Frags {
         bf16x8 v[B];
@@ -119,10 +127,16 @@ struct Part<true, B> {
         frag = r * 128 + (((lane >> 4) ^ (r >> 1)) & 7) * 16;
     }
     __device__ __forceinline__ void begin_slab(int) {}
+    // LAST: the slab may be the last one, whose chunks may lie beyond k
+    template <bool LAST>
     __device__ __forceinline__ void load(char *unit, int wave, int slab, int q) const
     {
         const int at = slab * (kSlab * 2);
-        load_to_lds(buffer, unit + (wave * LOADS + q) * 1024, at + chunk[q & 1] < k_bytes ? off[q] : (uint32_t)kOutside, at);
+        const uint32_t lane_off = !LAST || at + chunk[q & 1] < k_bytes ? off[q] : (uint32_t)kOutside;
+        if constexpr (BY_HAND)
+            load_to_lds_by_hand(buffer, unit + (wave * LOADS + q) * 1024, lane_off, at);
+        else
+            load_to_lds(buffer, unit + (wave * LOADS + q) * 1024, lane_off, at);
     }
     // read x of the fragments of K step kk
     __device__ __forceinline__ void read(const char *unit, int kk, int x, Frags &f) const
@@ -131,8 +145,8 @@ struct Part<true, B> {
     }
 };
 
-template <int B>
-struct Part<false, B> {
+template <int B, bool BY_HAND>
+struct Part<false, B, BY_HAND> {
     static constexpr int LOADS = B, READS = 2 * B, UNIT = 32 * B * 128;
     struct Frags {
         s16x4 v[2 * B];
@@ -169,9 +183,11 @@ struct Part<false, B> {
         const int64_t left = depth - (int64_t)slab * kSlab, lines = left < kSlab ? left : kSlab;
         buffer = raw_buffer(m + (int64_t)slab * kSlab * ld, (int)(((lines - 1) * ld + width) * 2));
     }
+    template <bool LAST>
     __device__ __forceinline__ void load(char *unit, int wave, int, int q) const
     {
-        load_to_lds(buffer, unit + (wave * LOADS + q) * 1024, off[q], 0);
+        static_assert(BY_HAND, "it is read by transposing reads");
+        load_to_lds_by_hand(buffer, unit + (wave * LOADS + q) * 1024, off[q], 0);
     }
     __device__ __forceinline__ void read(const char *unit, int kk, int x, Frags &f) const
     {
@@ -180,8 +196,9 @@ struct Part<false, B> {
     }
 };
 
-// Eight neighbouring columns of one row; `col` is a multiple of 8 and inside.
-__device__ __forceinline__ void finish8(const Epilogue<uint16_t> &ep, int64_t row, int64_t col, const float (&bias)[8], float (&v)[8])
+// Eight neighbouring columns of one row, with the chunks of mul and residual at hand; `col` is a multiple of 8 and inside.
+__device__ __forceinline__ void finish8(const Epilogue<uint16_t> &ep, int64_t row, int64_t col, const float (&bias)[8], const u32x4 &mul,
+                                        const u32x4 &residual, float (&v)[8])
 {
     typedef Chunk<uint16_t> C;
     float w[8];
@@ -198,13 +215,13 @@ __device__ __forceinline__ void finish8(const Epilogue<uint16_t> &ep, int64_t ro
             v[i] = act_value<true>(v[i], ep.act);
     }
     if (ep.mul) {
-        C::widen(*reinterpret_cast<const u32x4 *>(ep.mul + row * ep.ldm + col), w);
+        C::widen(mul, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             v[i] *= w[i];
     }
     if (ep.residual) {
-        C::widen(*reinterpret_cast<const u32x4 *>(ep.residual + row * ep.ldr + col), w);
+        C::widen(residual, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             v[i] += w[i];
@@ -215,8 +232,8 @@ __device__ __forceinline__ void finish8(const Epilogue<uint16_t> &ep, int64_t ro
 template <Product PRODUCT, int RB, int CB>
 __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16_t> a, const Epilogue<uint16_t> ep0, const TileOrder order)
 {
-    typedef Part<PRODUCT != kWeightGrad, RB> PartP;
-    typedef Part<PRODUCT == kForward, CB> PartQ;
+    typedef Part<PRODUCT != kWeightGrad, RB, PRODUCT != kForward> PartP;
+    typedef Part<PRODUCT == kForward, CB, PRODUCT != kForward> PartQ;
     constexpr int BR = 32 * RB, BC = 32 * CB;
     constexpr int NP = RB == 8 ? 3 : CB == 8 ? 4 : 5, NQ = RB == 8 ? 2 : CB == 8 ? 3 : 5, LEAD = NP - NQ;
     static_assert(NP * PartP::UNIT + NQ * PartQ::UNIT <= kLds && (LEAD == 0 || LEAD == 1), "the rings fit");
@@ -264,12 +281,12 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
     char *const p_ring = lds, *const q_ring = lds + NP * PartP::UNIT;
 
     // ---- the loads.  Iteration t (after the barrier of slab t) requests Q's slab t + NQ, then P's slab t + NP.
-    auto load_p = [&](int unit, int slab, int q) {
-        P.load(p_ring + unit * PartP::UNIT, wave, slab, q);
+    auto load_p = [&](int unit, int slab, int q, auto last) __attribute__((always_inline)) {
+        P.template load<decltype(last)::value>(p_ring + unit * PartP::UNIT, wave, slab, q);
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto load_q = [&](int unit, int slab, int q) {
-        Q.load(q_ring + unit * PartQ::UNIT, wave, slab, q);
+    auto load_q = [&](int unit, int slab, int q, auto last) __attribute__((always_inline)) {
+        Q.template load<decltype(last)::value>(q_ring + unit * PartQ::UNIT, wave, slab, q);
         __builtin_amdgcn_sched_barrier(0);
     };
     constexpr int AT_ONCE = (NL + 3) / 4;   // of an iteration's loads, those right after its barrier
@@ -279,7 +296,7 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
             P.begin_slab(slab);
 #pragma unroll
             for (int q = 0; q < PL; ++q)
-                load_p(slab % NP, slab, q);
+                load_p(slab % NP, slab, q, std::true_type{});
         }
     };
     if (LEAD == 1)
@@ -290,7 +307,7 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
             Q.begin_slab(t + NQ);
 #pragma unroll
             for (int q = 0; q < QL; ++q)
-                load_q(t + NQ, t + NQ, q);
+                load_q(t + NQ, t + NQ, q, std::true_type{});
         }
         all_p(t + NP);
     }
@@ -298,8 +315,18 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
         Q.begin_slab(NQ - 1);
 #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q)
-            load_q(NQ - 1, NQ - 1, q);
+            load_q(NQ - 1, NQ - 1, q, std::true_type{});
     }
+    // The sums stay in accumulation registers: cleared while the loads are on their way, and held there between slabs (left to
+    // itself the compiler moves some to and fro, or spills in the first slab).
+    auto pin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < CB; ++i)
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+                asm volatile("" : "+a"(acc[i][j]));
+    };
+    pin();
     // slab 0 has landed: all but the first part of P and of Q may be on their way
     auto begin = [&](auto slabs_tag) __attribute__((always_inline)) {
         constexpr int HAVE = decltype(slabs_tag)::value;   // slabs, at most NP
@@ -344,9 +371,11 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
     Frags f0, f1;
     for_each<0, READS>([&](auto x) __attribute__((always_inline)) { read_one(f0, 0, 0, 0, x); });
     int pu = 0, qu = 0, pu_old = NP - 1, qu_old = NQ - 1;   // ring places of slab s and of slab s - 1
-    // LEFT: how many slabs follow; NP stands for NP and more.
+    // LEFT: how many slabs follow; STEADY stands for that and more, and never requests the last slab.
+    constexpr int STEADY = LEAD == 0 ? NP + 1 : NP;
     auto slab_body = [&](int s, auto left_tag) __attribute__((always_inline)) {
         constexpr int LEFT = decltype(left_tag)::value;
+        constexpr auto LAST = std::integral_constant<bool, (LEFT < STEADY)>{};
         constexpr bool OLD_Q = LEFT >= NQ - 1, OLD_P = LEFT >= NP - 1, NEW_Q = LEFT >= NQ;   // what iterations s - 1 and s request
         const int pu1 = pu + 1 == NP ? 0 : pu + 1, qu1 = qu + 1 == NQ ? 0 : qu + 1;
         // what goes with instruction POS of the 2 N since a barrier: its share of the loads, in their order
@@ -356,9 +385,9 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
                 constexpr int X = decltype(x)::value;
                 if constexpr (X < QL) {
                     if constexpr (OLD_Q)
-                        load_q(qu_old, s - 1 + NQ, X);
+                        load_q(qu_old, s - 1 + NQ, X, LAST);
                 } else if constexpr (OLD_P) {
-                    load_p(pu_old, s - 1 + NP, X - QL);
+                    load_p(pu_old, s - 1 + NP, X - QL, LAST);
                 }
             });
         };
@@ -390,7 +419,7 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
             constexpr int I = decltype(n)::value;
             if constexpr (NEW_Q)
                 for_each<(I * NL + 2 * N - 1) / (2 * N), ((I + 1) * NL + 2 * N - 1) / (2 * N)>(
-                    [&](auto x) __attribute__((always_inline)) { load_q(qu, s + NQ, x); });
+                    [&](auto x) __attribute__((always_inline)) { load_q(qu, s + NQ, x, LAST); });
             if constexpr (LEFT > 0)
                 for_each<(I * READS + N / 2 - 1) / (N / 2), ((I + 1) * READS + N / 2 - 1) / (N / 2)>(
                     [&](auto x) __attribute__((always_inline)) { read_one(f0, pu1, qu1, 0, x); });
@@ -405,66 +434,85 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
     // (the first slab on its own: with one loop the compiler gives the accumulators other registers in every slab and moves
     // them back)
     int s = 0;
-    auto pin = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < CB; ++i)
-#pragma unroll
-            for (int j = 0; j < RB; ++j)
-                asm volatile("" : "+a"(acc[i][j]));
-    };
-    if (S > NP) {
-        slab_body(s++, std::integral_constant<int, NP>{});
+    if (S > STEADY) {
+        slab_body(s++, std::integral_constant<int, STEADY>{});
         pin();
-        for (; s + NP < S; ++s) {
-            slab_body(s, std::integral_constant<int, NP>{});
+        for (; s + STEADY < S; ++s) {
+            slab_body(s, std::integral_constant<int, STEADY>{});
             pin();
         }
     }
     auto last = [&](auto left_tag) {
         constexpr int LEFT = decltype(left_tag)::value;
-        if constexpr (LEFT < NP) {
-            if (s + LEFT < S)
+        if constexpr (LEFT < STEADY) {
+            if (s + LEFT < S) {
                 slab_body(s++, left_tag);
+                pin();
+            }
         }
     };
+    last(std::integral_constant<int, 5>{});
     last(std::integral_constant<int, 4>{});
     last(std::integral_constant<int, 3>{});
     last(std::integral_constant<int, 2>{});
     last(std::integral_constant<int, 1>{});
     last(std::integral_constant<int, 0>{});
     static_assert(NP <= 5, "every number of slabs left has its body");
-    block_barrier();   // the rings are about to be used again
     }
 
-    // ---- epilogue.  A wavefront passes 16 rows at a time through LDS of its own, as f32, so that a lane finishes eight
-    // neighbouring columns and rows are read and written in whole 128-byte lines.
+    // ---- epilogue.  A wavefront passes strips of 16 rows through LDS of its own, as f32, so that a lane finishes eight
+    // neighbouring columns and rows are read and written in whole 128-byte lines.  mul and residual are requested
+    // AHEAD strips before they are needed, the first while the last sums are still being finished.
     Epilogue<uint16_t> ep = ep0;
     if constexpr (PRODUCT == kWeightGrad)
         ep.out += (int64_t)expert * a.out_stride;
     constexpr int SROW = 16 * CB * 4 + 16, LANES = 2 * CB, ROWS = 64 / LANES;   // lanes of a row; rows of a read
+    constexpr int READS_16 = 16 / ROWS, AHEAD = 3;
     char *const strips = lds + wave * (kLds / 4);
     const int fr = lane & 15, g = lane >> 4;
-    const int64_t col = c0 + wc * 16 * CB + lane % LANES * 8;
+    const int64_t row0 = r0 + wr * 16 * RB + lane / LANES, col = c0 + wc * 16 * CB + lane % LANES * 8;
     float bias[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (ep.bias && col < ep.cols)
+    u32x4 mul[AHEAD + 1][READS_16], residual[AHEAD + 1][READS_16];
+    auto request = [&](auto j_tag) __attribute__((always_inline)) {
+        constexpr int J = decltype(j_tag)::value;
+        if constexpr (J < RB && PRODUCT == kForward) {
+#pragma unroll
+            for (int t = 0; t < READS_16; ++t) {
+                const int64_t r = row0 + J * 16 + t * ROWS;
+                if (r < r_end && col < ep.cols) {
+                    if (ep.mul)
+                        mul[J % (AHEAD + 1)][t] = *reinterpret_cast<const u32x4 *>(ep.mul + r * ep.ldm + col);
+                    if (ep.residual)
+                        residual[J % (AHEAD + 1)][t] = *reinterpret_cast<const u32x4 *>(ep.residual + r * ep.ldr + col);
+                }
+            }
+        }
+    };
+    for_each<0, AHEAD>(request);
+    if (PRODUCT == kForward && ep.bias && col < ep.cols)
         Chunk<uint16_t>::widen(*reinterpret_cast<const u32x4 *>(ep.bias + (int64_t)expert * ep.cols + col), bias);
+    block_barrier();   // the rings are about to be used again
     for_each<0, RB>([&](auto j_tag) __attribute__((always_inline)) {
-        constexpr int j = decltype(j_tag)::value;
-        char *const strip = strips + (j & 1) * 16 * SROW;
+        constexpr int J = decltype(j_tag)::value;
+        char *const strip = strips + (J & 1) * 16 * SROW;
+        request(std::integral_constant<int, J + AHEAD>{});
 #pragma unroll
         for (int i = 0; i < CB; ++i)
-            *reinterpret_cast<f32x4 *>(strip + fr * SROW + (i * 16 + 4 * g) * 4) = acc[i][j];
+            *reinterpret_cast<f32x4 *>(strip + fr * SROW + (i * 16 + 4 * g) * 4) = acc[i][J];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int t = 0; t < 16 / ROWS; ++t) {
-            const int row = t * ROWS + lane / LANES;
-            const f32x4 lo = *reinterpret_cast<const f32x4 *>(strip + row * SROW + lane % LANES * 32);
-            const f32x4 hi = *reinterpret_cast<const f32x4 *>(strip + row * SROW + lane % LANES * 32 + 16);
+        for (int t = 0; t < READS_16; ++t) {
+            const char *at = strip + (t * ROWS + lane / LANES) * SROW + lane % LANES * 32;
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(at), hi = *reinterpret_cast<const f32x4 *>(at + 16);
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            const int64_t r = r0 + wr * 16 * RB + j * 16 + row;
-            if (r < r_end && col < ep.cols)
-                finish8(ep, r, col, bias, v);
+            const int64_t r = row0 + J * 16 + t * ROWS;
+            if (r < r_end && col < ep.cols) {
+                if constexpr (PRODUCT == kForward)
+                    finish8(ep, r, col, bias, mul[J % (AHEAD + 1)][t], residual[J % (AHEAD + 1)][t], v);
+                else
+                    *reinterpret_cast<u32x4 *>(ep.out + r * ep.ldo + col) = Chunk<uint16_t>::narrow(v);
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
