@@ -417,6 +417,8 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  *   pre_out  NULL or [T, d_out]: pre, as the gradient needs it
  *   out      [T, d_out]; may be mul or residual itself (same stride), but no
  *            other operand
+ *   workspace  dass_linear_workspace_bytes() bytes, 16-byte aligned (0 and NULL
+ *            where the outputs are many; else partial sums over shares of d_in)
  * All of dtype dt (bf16 or f32); sums and epilogue are f32, rounded once (pre
  * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32), T below 2^31.
  *
@@ -455,7 +457,11 @@ typedef struct {
     dass_act act;
 } dass_linear_task;
 
-dass_status dass_linear(const dass_linear_task *task, void *hip_stream);
+size_t dass_linear_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt,
+                                   int64_t n_experts);
+
+dass_status dass_linear(const dass_linear_task *task, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
 
 typedef struct {
     const void *dout;

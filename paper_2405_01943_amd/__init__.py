@@ -10,7 +10,7 @@ from .binding import (  # noqa: F401
     input_norms, input_norms_workspace_bytes,
     mlp_forward, mlp_forward_workspace_bytes, compress_24, down_proj_sparse24,
     expert_sort, expert_sort_workspace_bytes, expert_gather, expert_combine, expert_combine_backward,
-    linear, linear_backward, linear_backward_workspace_bytes,
+    linear, linear_workspace_bytes, linear_backward, linear_backward_workspace_bytes,
     score_mask_nm, nm_workspace_bytes,
     score_mask_nm_batched, nm_batched_workspace_bytes,
     score_mask_unstructured, score_mask_unstructured_static, unstructured_workspace_bytes,

@@ -31,7 +31,7 @@ EXPORTS = (
     "dass_mlp_forward_workspace_bytes", "dass_mlp_forward", "dass_compress_24", "dass_down_proj_sparse24",
     "dass_expert_sort_workspace_bytes", "dass_expert_sort", "dass_expert_gather", "dass_expert_combine",
     "dass_expert_combine_backward",
-    "dass_linear", "dass_linear_backward_workspace_bytes", "dass_linear_backward",
+    "dass_linear_workspace_bytes", "dass_linear", "dass_linear_backward_workspace_bytes", "dass_linear_backward",
     "dass_status_string", "dass_last_error_string", "dass_version",
 )
 
@@ -142,7 +142,9 @@ def load_library() -> ctypes.CDLL:
     lib.dass_expert_combine_backward.restype = ci
     lib.dass_expert_combine_backward.argtypes = [vp, i64, vp, i64, vp, i64, i64, vp, i64, ci, vp, i64, vp, vp]
     lib.dass_linear.restype = ci
-    lib.dass_linear.argtypes = [ctypes.POINTER(LinearTask), vp]
+    lib.dass_linear.argtypes = [ctypes.POINTER(LinearTask), vp, sz, vp]
+    lib.dass_linear_workspace_bytes.restype = sz
+    lib.dass_linear_workspace_bytes.argtypes = [i64, i64, i64, ci, i64]
     lib.dass_linear_backward_workspace_bytes.restype = sz
     lib.dass_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, ci, i64]
     lib.dass_linear_backward.restype = ci
@@ -621,9 +623,14 @@ def _bias(t: Optional[torch.Tensor], name: str, n_experts: int, d_out: int, dtyp
         raise TypeError(f"{name}: need contiguous {'[n_experts, d_out]' if n_experts else '[d_out]'} in the dtype of X")
 
 
+def linear_workspace_bytes(T: int, d_in: int, d_out: int, dtype: torch.dtype, n_experts: int = 1) -> int:
+    return int(load_library().dass_linear_workspace_bytes(T, d_in, d_out, DTYPE[dtype], n_experts))
+
+
 def linear(X: torch.Tensor, W: torch.Tensor, out: torch.Tensor, act: str = "none", bias: Optional[torch.Tensor] = None,
            mul: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
-           pre_out: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, stream=None) -> None:
+           pre_out: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """dass_linear: out = act(X W^T + bias) * mul + residual.
 
     Dense: W [d_out, d_in], bias [d_out].  By expert: offsets int32[n_experts + 1] (as expert_sort leaves
@@ -640,10 +647,14 @@ def linear(X: torch.Tensor, W: torch.Tensor, out: torch.Tensor, act: str = "none
     ldm, ldr = _like(mul, "mul", shape, dt), _like(residual, "residual", shape, dt)
     ldp, ldo = _like(pre_out, "pre_out", shape, dt), _like(out, "out", shape, dt)
     _bias(bias, "bias", E, d_out, dt)
-    _on_device(stream, X, W, out, bias, mul, residual, pre_out, offsets)
+    _on_device(stream, X, W, out, bias, mul, residual, pre_out, offsets, workspace)
+    if workspace is None:
+        need = int(lib.dass_linear_workspace_bytes(T, d_in, d_out, DTYPE[dt], max(E, 1)))
+        if need > 0:
+            workspace = _scratch(need, X.device, stream)
     task = LinearTask(_ptr(X), T, ldx, _ptr(W), ldw, per_expert, d_in, d_out, _ptr(offsets), max(E, 1), _ptr(bias), _ptr(mul),
                       ldm, _ptr(residual), ldr, _ptr(pre_out), ldp, _ptr(out), ldo, DTYPE[dt], code)
-    status = lib.dass_linear(ctypes.byref(task), _stream(stream))
+    status = lib.dass_linear(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), _stream(stream))
     if status:
         _check(status)
 

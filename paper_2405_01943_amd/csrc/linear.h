@@ -6,6 +6,8 @@
 #include "chunk.h"
 #include "dass_internal.h"
 
+#include <type_traits>
+
 namespace dass {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -138,10 +140,35 @@ struct Operands {
     Segments seg;
 };
 
-// One launch each; errors as the entry points report them.
-dass_status launch_product_f32(const char *fn, Product product, const Operands<float> &a, const Epilogue<float> &ep,
-                               hipStream_t stream);
-dass_status launch_product_bf16(const char *fn, Product product, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,
-                                hipStream_t stream);
+// Shares of k that the launch's third dimension takes apart: each writes its sums, f32 [rows of the output][cols], to
+// partial + share * stride.  n = 1: no split.
+struct Split {
+    float *partial;
+    int64_t stride;
+    int n;
+};
+
+// Which kernel a product takes (plan_product in linear.hip).
+struct Plan {
+    enum Kind { kTiles, kFew } kind;
+    int tile;     // kTiles: 0: 256 x 256, 1: 128 x 256, 2: 128 x 128 (f32: always 2)
+    int splits;   // kTiles: shares of k
+    int blocks;   // kFew: 16-row (and in f32 16-column) blocks of a workgroup
+};
+
+// One launch each, two with split k; errors as the entry points report them.
+#define DASS_DECLARE_TILES(name)                                                                                              \
+    dass_status name(const char *fn, const Plan &plan, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,             \
+                     const Split &split, hipStream_t stream);                                                                 \
+    dass_status name(const char *fn, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep, const Split &split, \
+                     hipStream_t stream);
+DASS_DECLARE_TILES(launch_forward)
+DASS_DECLARE_TILES(launch_dx)
+DASS_DECLARE_TILES(launch_dw)
+#undef DASS_DECLARE_TILES
+dass_status launch_few(const char *fn, Product product, const Plan &plan, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,
+                       hipStream_t stream);
+dass_status launch_few(const char *fn, Product product, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep,
+                       hipStream_t stream);
 
 }  // namespace dass

@@ -1,12 +1,14 @@
 // dass_linear: out = act(X W^T + b) * mul + residual, with one W for all rows or that of each row's expert, and its
 // gradients.  This file has the checks, the element-wise part of the gradient and the bias sums; the products are in
-// linear_bf16.hip and linear_f32.hip.
+// linear_tiles.h and linear_few.hip.
 //
 // Gradients, with g = dout * mul * act'(pre):  dX = g W,  dW = g^T X over an expert's rows,  db = sum of its g,
 // dmul = dout * act(pre).  g is read by both products, so it is written once, in dtype dt: rounded to bf16
 // there because the matrix cores take nothing wider (each term of a sum is off by half a step of its own, which adds about as
 // much to a sum as its own rounding does).  Without activation and mul, g is dout itself and nothing is written.
 #include "linear.h"
+
+#include <algorithm>
 
 namespace dass {
 
@@ -186,17 +188,110 @@ struct Checker {
     }
 };
 
-template <typename T_>
-static dass_status launch_product(const char *fn, Product product, const Operands<T_> &a, const Epilogue<T_> &ep, hipStream_t stream)
+// The kernel, the tile and the split of k that are expected to be fastest for the products of `groups` experts: cols columns,
+// `depth` of k each, and `rows` rows each (dW) or all together.  The estimates, in us, are lines through times of 90 bf16 and 45
+// f32 products of 1 to 16384 rows and every tile with 1 to 16 shares; over these the choice is 1 % slower than the best in
+// the mean, 31 % at the worst (dX of 16 rows an expert).
+//
+//   tiles   rounds of 256 workgroups x (start + slabs x slab), and with a split 8 bytes for each share's sum (written and
+//           read) and the second launch.  A tile's slab takes as long as its bytes from L2, whichever shape; large
+//           tiles read least in all, small ones and shares fill the chip.  1024 rows of 4096 x 4096, 256 x 256 / 128 x
+//           256 / 128 x 128: 93 / 56 / 39 us, 52 / 46 / 55 with 4, 2 and 2 shares; 16384 rows of 4096 x 11008: 1197 us with
+//           256 x 256; dX of 6000 rows of 4096 x 11008 473 / 503 / -; 64 rows of 11008 x 4096 (128 x 128) 88 us, 27 with 8 shares; dW of 16384 rows of 512 x 512 145, 28
+//           with 8; one share where the tiles fill the chip: 2048 rows of 4096 x 4096 59 us, 86 with 2.
+//   few     (f32) a fixed part that grows with k, or the workgroups and their multiplications.  512 rows of 256 x 688: blocks
+//           of 16 / of 32 / tiles 14.5 / 8.1 / 16.6 us, 16 of 1024 x 1024 9.3 / 14.0 / 11.5, 2048 of 512 x 512 32 / 19 / 27,
+//           4096 of 1024 x 1024 225 / 119 / 71.
+//           (bf16, forward only) up to 8 rows where 128 x 128 tiles leave compute units idle, and one row an expert: one row of
+//           4096 x 11008 19.5 us (tiles with 4 shares 24), 8 of it 22.9 (24), 16 of it 27 (24); 8 rows over 5 experts of 4096 x
+//           14336 98 (130), but 16 over 8 170 (163).
+static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, int64_t cols, int64_t depth)
 {
-    if constexpr (sizeof(T_) == 2)
-        return launch_product_bf16(fn, product, a, ep, stream);
-    else
-        return launch_product_f32(fn, product, a, ep, stream);
+    const bool bf16 = dt == DASS_BF16;
+    const auto pieces = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
+    const int64_t share = product == kWeightGrad ? rows : pieces(rows, groups);   // of an expert, were they even
+    if (bf16 && product == kForward && (share == 1 || (share <= 8 && groups * pieces(cols, 128) < 256)))
+        return {Plan::kFew, 0, 1, 1};
+    // the row tiles of experts of uneven size: half a tile more each
+    const auto row_tiles = [&](int64_t of) {
+        if (product == kWeightGrad || groups == 1)
+            return groups * pieces(rows, of);
+        return std::max(groups, rows / of + groups / 2);
+    };
+
+    static const int kShares[] = {1, 2, 3, 4, 6, 8, 12, 16};
+    static const struct {
+        int rows, cols;
+        double start, slab;
+    } kTiles[] = {{256, 256, 5.4, 1.0}, {128, 256, 3.3, 0.67}, {128, 128, 1.9, 0.435}}, kTileF32 = {128, 128, 3.4, 2.49};
+    const double join = bf16 ? 4.4 : 2.4, byte = bf16 ? 1 / 6.9e6 : 1 / 4.5e6;   // us, us a byte
+    const int64_t slabs = pieces(depth, bf16 ? 64 : 32), outputs = (product == kWeightGrad ? groups : 1) * rows * cols;
+    Plan best = {Plan::kTiles, bf16 ? 0 : 2, 1, 0};
+    double best_time = 1e300;
+    for (int k = bf16 ? 0 : 2; k < 3; ++k) {
+        const auto &t = bf16 ? kTiles[k] : kTileF32;
+        const int64_t tiles = row_tiles(t.rows) * pieces(cols, t.cols);
+        for (const int z : kShares) {
+            if (z > 1 && (slabs < 2 * z || (double)z * outputs * 4 > 256e6))
+                break;
+            const double time = pieces(tiles * z, 256) * (t.start + pieces(slabs, z) * t.slab) + (z > 1 ? join + z * 8.0 * outputs * byte : 0);
+            if (time < best_time) {
+                best_time = time;
+                best = {Plan::kTiles, k, z, 0};
+            }
+        }
+    }
+    for (int blocks = 1; !bf16 && blocks <= 2; ++blocks) {
+        const double groups_of_4 = (double)row_tiles(16 * blocks) * pieces(cols, 16 * blocks);
+        const double fixed = blocks == 1 ? 7 + 0.0022 * depth : 6.5 + 0.0075 * depth;
+        const double busy = 5 + groups_of_4 * (0.006 + (blocks == 1 ? 28e-9 : 20.7e-9) * 256 * blocks * blocks * depth);
+        if (fixed < best_time && busy < best_time) {
+            best_time = fixed > busy ? fixed : busy;
+            best = {Plan::kFew, 0, 1, blocks};
+        }
+    }
+    return best;
+}
+
+static Plan plan_of(Product product, int dt, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+{
+    if (product == kForward)
+        return plan_product(product, dt, n_experts, T, d_out, d_in);
+    if (product == kInputGrad)
+        return plan_product(product, dt, n_experts, T, d_in, d_out);
+    return plan_product(product, dt, n_experts, d_out, d_in, (T + n_experts - 1) / n_experts);
+}
+
+static int64_t output_size(Product product, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+{
+    return product == kForward ? T * d_out : product == kInputGrad ? T * d_in : n_experts * d_out * d_in;
+}
+
+static size_t split_bytes(Product product, int dt, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+{
+    const Plan plan = plan_of(product, dt, T, d_in, d_out, n_experts);
+    return plan.splits > 1 ? round_up((size_t)plan.splits * output_size(product, T, d_in, d_out, n_experts) * 4, 256) : 0;
 }
 
 template <typename T_>
-static dass_status run_linear(const char *fn, const dass_linear_task &t, hipStream_t stream)
+static dass_status launch_product(const char *fn, Product product, int64_t d_in, int64_t d_out, const Operands<T_> &a, const Epilogue<T_> &ep,
+                                  void *workspace, hipStream_t stream)
+{
+    const int dt = sizeof(T_) == 2 ? DASS_BF16 : DASS_F32;
+    const Plan plan = plan_of(product, dt, a.seg.rows, d_in, d_out, a.seg.n);
+    if (plan.kind == Plan::kFew)
+        return launch_few(fn, product, plan, a, ep, stream);
+    // 32-bit byte offsets inside a tile: 256 rows (by rows), a slab's lines (k by k)
+    if (256 * a.ldp * (int64_t)sizeof(T_) >= 0x7fffffffLL || 256 * a.ldq * (int64_t)sizeof(T_) >= 0x7fffffffLL)
+        return fail(DASS_ERR_SHAPE, "%s: rows too long for the tile addressing", fn);
+    const Split split = {static_cast<float *>(workspace), output_size(product, a.seg.rows, d_in, d_out, a.seg.n), plan.splits};
+    if (product == kForward)
+        return launch_forward(fn, plan, a, ep, split, stream);
+    return product == kInputGrad ? launch_dx(fn, plan, a, ep, split, stream) : launch_dw(fn, plan, a, ep, split, stream);
+}
+
+template <typename T_>
+static dass_status run_linear(const char *fn, const dass_linear_task &t, void *workspace, hipStream_t stream)
 {
     Operands<T_> a = {};
     a.P = static_cast<const T_ *>(t.X);
@@ -209,7 +304,7 @@ static dass_status run_linear(const char *fn, const dass_linear_task &t, hipStre
     const Epilogue<T_> ep = {static_cast<T_ *>(t.out), t.ldo, static_cast<const T_ *>(t.bias), static_cast<const T_ *>(t.mul),
                              t.ldm, static_cast<const T_ *>(t.residual), t.ldr, static_cast<T_ *>(t.pre_out), t.ldp, t.d_out,
                              (int)t.act};
-    return launch_product(fn, kForward, a, ep, stream);
+    return launch_product(fn, kForward, t.d_in, t.d_out, a, ep, workspace, stream);
 }
 
 template <typename T_>
@@ -220,6 +315,8 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     const bool own_g = (t.act != DASS_ACT_NONE || t.mul) && (t.dX || t.dW);
     const T_ *g = static_cast<const T_ *>(t.dout);
     int64_t ldg = t.ldg;
+    // the workspace: g, then the partial sums of the bias, whose place the split products take after them
+    char *const shares = workspace + kept_bytes(t.T, t.d_out, t.dt);
     if (own_g || t.dbias || t.dmul) {
         T_ *kept = own_g ? reinterpret_cast<T_ *>(workspace) : nullptr;
         float *partial = t.dbias ? reinterpret_cast<float *>(workspace + kept_bytes(t.T, t.d_out, t.dt)) : nullptr;
@@ -260,7 +357,7 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
         ep.ldo = t.lddx;
         ep.cols = t.d_in;
         ep.act = DASS_ACT_NONE;
-        const dass_status s = launch_product(fn, kInputGrad, a, ep, stream);
+        const dass_status s = launch_product(fn, kInputGrad, t.d_in, t.d_out, a, ep, shares, stream);
         if (s != DASS_OK)
             return s;
     }
@@ -278,14 +375,22 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
         ep.ldo = t.lddw;
         ep.cols = t.d_in;
         ep.act = DASS_ACT_NONE;
-        return launch_product(fn, kWeightGrad, a, ep, stream);
+        return launch_product(fn, kWeightGrad, t.d_in, t.d_out, a, ep, shares, stream);
     }
     return DASS_OK;
 }
 
 }  // namespace dass
 
-extern "C" dass_status dass_linear(const dass_linear_task *task, void *hip_stream)
+extern "C" size_t dass_linear_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
+{
+    using namespace dass;
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL)
+        return 0;
+    return split_bytes(kForward, dt, T, d_in, d_out, n_experts);
+}
+
+extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     using namespace dass;
     const char *fn = "dass_linear";
@@ -304,16 +409,26 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *hip_strea
     c.stride("W", t.expert_stride, t.ldw, t.d_in, t.d_out, t.n_experts);
     if (c.status != DASS_OK)
         return c.status;
+    const size_t need = dass_linear_workspace_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(DASS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
+    if (need > 0 && !aligned16(workspace))
+        return fail(DASS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", fn);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return t.dt == DASS_BF16 ? run_linear<uint16_t>(fn, t, stream) : run_linear<float>(fn, t, stream);
+    return t.dt == DASS_BF16 ? run_linear<uint16_t>(fn, t, workspace, stream) : run_linear<float>(fn, t, workspace, stream);
 }
 
 extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
     using namespace dass;
-    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt))
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL)
         return 0;
-    return kept_bytes(T, d_out, dt) + partial_bytes(T, d_out, n_experts);
+    size_t shares = partial_bytes(T, d_out, n_experts);
+    for (const Product p : {kInputGrad, kWeightGrad}) {
+        const size_t b = split_bytes(p, dt, T, d_in, d_out, n_experts);
+        shares = b > shares ? b : shares;
+    }
+    return kept_bytes(T, d_out, dt) + shares;
 }
 
 extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, void *workspace, size_t workspace_bytes,

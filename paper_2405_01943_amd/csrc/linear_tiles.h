@@ -1,17 +1,20 @@
-// dass_linear and dass_linear_backward in bf16 on the matrix cores.
+// The products of dass_linear and dass_linear_backward on the matrix cores, tile by tile (bf16 and f32).
 //
 // A workgroup owns a tile of 32 RB rows x 32 CB columns of the output, its four wavefronts (2 x 2) a quarter each:
-// RB x CB blocks of v_mfma_f32_16x16x32_bf16, for 8 x 8 all 256 accumulation registers of a lane.  Slabs of 64 k go
+// RB x CB blocks of 16 x 16, for 8 x 8 all 256 accumulation registers of a lane.  Slabs of 128 bytes of k (64 bf16, 32 f32) go
 // from global memory straight into LDS (16 bytes a lane, no registers in between).  Output columns are the
-// instruction's M index and rows its N index, so a lane holds four neighbouring columns of a row.
+// instruction's M index and rows its N index, so a lane holds four neighbouring columns of a row.  bf16:
+// v_mfma_f32_16x16x32_bf16; f32: four v_mfma_f32_16x16x4_f32, the i-th on the i-th of the four k that a lane holds of a row, so
+// that it covers k = i, 4 + i, 8 + i, 12 + i of both operands.
 //
 // An operand comes in one of two forms, and LDS holds it in the form that it has in memory:
-//   by rows   a wave-load is 8 rows x 128 bytes; a lane's eight k of a row are one 16-byte read.  16-byte chunk c of
+//   by rows   a wave-load is 8 rows x 128 bytes; a lane's 16 bytes of a row are one read.  16-byte chunk c of
 //             row r lies in slot c ^ (r / 2 mod 8): 16 rows of one chunk meet 16 places of the banks.
-//   k by k    a wave-load is 2 (4) lines of k of 256 (128) rows.  ds_read_b64_tr_b16 reads a 4 x 16 block of k x rows for 16
+//   k by k    a wave-load is 1 KB of lines of k.  bf16: ds_read_b64_tr_b16 reads a 4 x 16 block of k x rows for 16
 //             lanes and gives each lane the four k of one row; two of them are a lane's eight k.  A block's 32 bytes
 //             of line k lie in place piece ^ f(k), f(k) = (k mod 4) + 4 (k / 8 mod 2), so that the eight lines
-//             that 32 lanes read at a time meet all 64 banks once.
+//             that 32 lanes read at a time meet all 64 banks once.  f32: a lane's four k are four reads of 4 bytes; a block's 64
+//             bytes of line k lie in place piece ^ (k / 4 mod 4), so that the four lines of a read meet all banks once.
 // So no operand is transposed in memory: the three products (linear.h) differ in their operands' forms alone.
 //
 // LDS is two rings, NP parts of P and NQ of Q, as many as 160 KB hold.  The places of slab s are free after the one
@@ -24,9 +27,15 @@
 // valid element; what lies beyond reads as 0.  Lane offsets are 32-bit registers, the scalar offset is at most a row
 // (by rows) or none (k by k, whose buffer moves with the slab), so the length less the scalar offset is never negative.  By rows, chunks of
 // the last slab that lie beyond k are given an offset outside the buffer.
+//
+// Grids of few tiles split k over blockIdx.z: each share writes its sums as f32 to a place of its own in the workspace, and a second
+// launch adds them up in order and finishes the outputs (join_kernel).
+#pragma once
+
 #include "linear.h"
 #include "tile_order.h"
 
+#include <cstdlib>
 #include <type_traits>
 #include <utility>
 
@@ -52,7 +61,7 @@ __device__ __forceinline__ void for_each(F &&f)
                     std::make_integer_sequence<int, TO - FROM>{});
 }
 
-constexpr int kLds = 160 * 1024, kSlab = 64;
+constexpr int kLds = 160 * 1024, kSlabBytes = 128;
 constexpr int kOutside = 0x7fffffff;
 
 // A raw buffer: 48 bits of address, no stride, its length in bytes.
@@ -78,7 +87,7 @@ __device__ __forceinline__ void load_to_lds_by_hand(const u32x4 &buffer, char *d
 {
     const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr_t)dst;
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(lane_off), "s"(buffer),
-                 "s"(off) : "m0", "memory");
+                 "s"(off) : "memory");
 }
 
 __device__ __forceinline__ void block_barrier()
@@ -97,32 +106,31 @@ __device__ __forceinline__ void wait_loads()
 }
 
 // One operand of a workgroup: its loads into LDS and its fragments from there.  B: blocks of 16 rows of a wavefront.
-template <bool BY_ROWS, int B, bool BY_HAND>
+template <typename T_, bool BY_ROWS, int B, bool BY_HAND>
 struct Part;
 
-template <int B, bool BY_HAND>
-struct Part<true, B, BY_HAND> {
-    static constexpr int LOADS = B, READS = B, UNIT = 32 * B * 128;
+template <typename T_, int B, bool BY_HAND>
+struct Part<T_, true, B, BY_HAND> {
+    static constexpr int LOADS = B, READS = B, UNIT = 32 * B * 128, E = sizeof(T_);
     struct Frags {
-        bf16x8 v[B];
-        __device__ __forceinline__ bf16x8 get(int b) const { return v[b]; }
+        u32x4 v[B];
+        __device__ __forceinline__ u32x4 get(int b) const { return v[b]; }
     };
     u32x4 buffer;
     uint32_t off[LOADS];
     int chunk[2], k_bytes, frag;
 
-    __device__ __forceinline__ void init(const uint16_t *m, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane,
-                                         int part)
+    __device__ __forceinline__ void init(const T_ *m, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane, int part)
     {
         const int64_t n = rows - row0 < 32 * B ? rows - row0 : 32 * B;
-        buffer = raw_buffer(m + row0 * ld + k0, (int)(((n - 1) * ld + k) * 2));
-        k_bytes = (int)(k * 2);
+        buffer = raw_buffer(m + row0 * ld + k0, (int)(((n - 1) * ld + k) * E));
+        k_bytes = (int)(k * E);
         const int sub = lane >> 3;
         chunk[0] = ((lane & 7) ^ (sub >> 1)) * 16;
         chunk[1] = chunk[0] ^ 64;                          // rows 8 further on: r / 2 has changed by 4
 #pragma unroll
         for (int q = 0; q < LOADS; ++q)
-            off[q] = (uint32_t)(((wave * LOADS + q) * 8 + sub) * ld * 2) + chunk[q & 1];
+            off[q] = (uint32_t)(((wave * LOADS + q) * 8 + sub) * ld * E) + chunk[q & 1];
         const int r = part * 16 * B + (lane & 15);
         frag = r * 128 + (((lane >> 4) ^ (r >> 1)) & 7) * 16;
     }
@@ -131,7 +139,7 @@ struct Part<true, B, BY_HAND> {
     template <bool LAST>
     __device__ __forceinline__ void load(char *unit, int wave, int slab, int q) const
     {
-        const int at = slab * (kSlab * 2);
+        const int at = slab * kSlabBytes;
         const uint32_t lane_off = !LAST || at + chunk[q & 1] < k_bytes ? off[q] : (uint32_t)kOutside;
         if constexpr (BY_HAND)
             load_to_lds_by_hand(buffer, unit + (wave * LOADS + q) * 1024, lane_off, at);
@@ -141,30 +149,24 @@ struct Part<true, B, BY_HAND> {
     // read x of the fragments of K step kk
     __device__ __forceinline__ void read(const char *unit, int kk, int x, Frags &f) const
     {
-        f.v[x] = *reinterpret_cast<const bf16x8 *>(unit + (frag ^ (kk * 64)) + x * 2048);
+        f.v[x] = *reinterpret_cast<const u32x4 *>(unit + (frag ^ (kk * 64)) + x * 2048);
     }
 };
 
-template <int B, bool BY_HAND>
-struct Part<false, B, BY_HAND> {
-    static constexpr int LOADS = B, READS = 2 * B, UNIT = 32 * B * 128;
-    struct Frags {
-        s16x4 v[2 * B];
-        __device__ __forceinline__ bf16x8 get(int b) const
-        {
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[2 * b], v[2 * b + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-    };
-    static constexpr int LINE = 32 * B * 2, SLOTS = LINE / 16, LINES = 1024 / LINE;   // bytes, chunks; lines of a wave-load
-    const uint16_t *m;
+// The lines of k of an operand that is stored k by k.
+template <typename T_, int B, bool BY_HAND>
+struct Lines {
+    static constexpr int LOADS = B, UNIT = 32 * B * 128, E = sizeof(T_), SLAB = kSlabBytes / E;
+    static constexpr int LINE = 32 * B * E, SLOTS = LINE / 16, LINES = 1024 / LINE;   // bytes, chunks; lines of a wave-load
+    static_assert(LINES * LINE == 1024 && LINES > 0, "whole lines");
+    const T_ *m;
     int64_t ld, depth, width;
     u32x4 buffer;
     uint32_t off[LOADS];
-    int frag;
 
-    static __device__ __forceinline__ int f_of(int k) { return (k & 3) | (k >> 1 & 4); }
-    __device__ __forceinline__ void init(const uint16_t *base, int64_t ld_, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane,
-                                         int part)
+    // swap(line): what the place of a 16-byte chunk is XORed with
+    template <typename F>
+    __device__ __forceinline__ void init_lines(const T_ *base, int64_t ld_, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane, F swap)
     {
         m = base + k0 * ld_ + row0;
         ld = ld_;
@@ -172,68 +174,131 @@ struct Part<false, B, BY_HAND> {
         width = rows - row0 < 32 * B ? rows - row0 : 32 * B;
 #pragma unroll
         for (int q = 0; q < LOADS; ++q) {
-            const int line = wave * 16 + q * LINES + lane / SLOTS;
-            off[q] = (uint32_t)(line * ld * 2) + ((lane % SLOTS) ^ (f_of(line) << 1)) * 16;
+            const int line = (wave * LOADS + q) * LINES + lane / SLOTS;
+            off[q] = (uint32_t)(line * ld * E) + ((lane % SLOTS) ^ swap(line)) * 16;
         }
-        const int g = lane >> 4, i = lane & 15, line = 8 * g + (i >> 2);
-        frag = line * LINE + (((part * B) ^ f_of(line)) * 32) + (i & 3) * 8;
     }
     __device__ __forceinline__ void begin_slab(int slab)
     {
-        const int64_t left = depth - (int64_t)slab * kSlab, lines = left < kSlab ? left : kSlab;
-        buffer = raw_buffer(m + (int64_t)slab * kSlab * ld, (int)(((lines - 1) * ld + width) * 2));
+        const int64_t left = depth - (int64_t)slab * SLAB, lines = left < SLAB ? left : SLAB;
+        buffer = raw_buffer(m + (int64_t)slab * SLAB * ld, (int)(((lines - 1) * ld + width) * E));
     }
     template <bool LAST>
     __device__ __forceinline__ void load(char *unit, int wave, int, int q) const
     {
-        static_assert(BY_HAND, "it is read by transposing reads");
-        load_to_lds_by_hand(buffer, unit + (wave * LOADS + q) * 1024, off[q], 0);
+        if constexpr (BY_HAND)
+            load_to_lds_by_hand(buffer, unit + (wave * LOADS + q) * 1024, off[q], 0);
+        else
+            load_to_lds(buffer, unit + (wave * LOADS + q) * 1024, off[q], 0);
+    }
+};
+
+template <int B, bool BY_HAND>
+struct Part<uint16_t, false, B, BY_HAND> : Lines<uint16_t, B, BY_HAND> {
+    static_assert(BY_HAND, "it is read by transposing reads");
+    typedef Lines<uint16_t, B, BY_HAND> Base;
+    static constexpr int READS = 2 * B;
+    struct Frags {
+        s16x4 v[2 * B];
+        __device__ __forceinline__ u32x4 get(int b) const
+        {
+            return __builtin_bit_cast(u32x4, __builtin_shufflevector(v[2 * b], v[2 * b + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    };
+    int frag;
+
+    static __device__ __forceinline__ int f_of(int k) { return (k & 3) | (k >> 1 & 4); }
+    __device__ __forceinline__ void init(const uint16_t *base, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane, int part)
+    {
+        this->init_lines(base, ld, row0, rows, k0, k, wave, lane, [](int line) { return f_of(line) << 1; });
+        const int g = lane >> 4, i = lane & 15, line = 8 * g + (i >> 2);
+        frag = line * Base::LINE + (((part * B) ^ f_of(line)) * 32) + (i & 3) * 8;
     }
     __device__ __forceinline__ void read(const char *unit, int kk, int x, Frags &f) const
     {
         f.v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4_t)(unit + (frag ^ (x / 2 * 32)) + (x % 2 * 4 + kk * 32) * LINE));
+            (lds_s16x4_t)(unit + (frag ^ (x / 2 * 32)) + (x % 2 * 4 + kk * 32) * Base::LINE));
     }
 };
 
-// Eight neighbouring columns of one row, with the chunks of mul and residual at hand; `col` is a multiple of 8 and inside.
-__device__ __forceinline__ void finish8(const Epilogue<uint16_t> &ep, int64_t row, int64_t col, const float (&bias)[8], const u32x4 &mul,
-                                        const u32x4 &residual, float (&v)[8])
+template <int B, bool BY_HAND>
+struct Part<float, false, B, BY_HAND> : Lines<float, B, BY_HAND> {
+    typedef Lines<float, B, BY_HAND> Base;
+    static constexpr int READS = 4 * B;
+    struct Frags {
+        uint32_t v[4 * B];
+        __device__ __forceinline__ u32x4 get(int b) const { return u32x4{v[4 * b], v[4 * b + 1], v[4 * b + 2], v[4 * b + 3]}; }
+    };
+    int frag;
+
+    static __device__ __forceinline__ int f_of(int k) { return k >> 2 & 3; }
+    __device__ __forceinline__ void init(const float *base, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane, int part)
+    {
+        this->init_lines(base, ld, row0, rows, k0, k, wave, lane, [](int line) { return f_of(line) << 2; });
+        const int g = lane >> 4, line = 4 * g;
+        frag = line * Base::LINE + (((part * B) ^ f_of(line)) * 64) + (lane & 15) * 4;
+    }
+    __device__ __forceinline__ void read(const char *unit, int kk, int x, Frags &f) const
+    {
+        f.v[x] = *reinterpret_cast<const uint32_t *>(unit + (frag ^ (x / 4 * 64)) + (x % 4 + kk * 16) * Base::LINE);
+    }
+};
+
+__device__ __forceinline__ f32x4 multiply_add(const u32x4 &q, const u32x4 &p, const f32x4 &acc, uint16_t)
 {
-    typedef Chunk<uint16_t> C;
-    float w[8];
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, p), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply_add(const u32x4 &q, const u32x4 &p, f32x4 acc, float)
+{
+    const f32x4 a = __builtin_bit_cast(f32x4, q), b = __builtin_bit_cast(f32x4, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc, 0, 0, 0);
+    return acc;
+}
+
+// The epilogue of one 16-byte chunk of a row (8 bf16, 4 f32), with the chunks of mul and residual at hand; `col` is inside.
+template <typename T_, int N = Chunk<T_>::N>
+__device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int64_t col, const float (&bias)[N], const u32x4 &mul,
+                                       const u32x4 &residual, float (&v)[N])
+{
+    typedef Chunk<T_> C;
+    constexpr bool FAST = sizeof(T_) == 2;
+    float w[N];
     if (ep.bias) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
             v[i] += bias[i];
     }
     if (ep.pre)
         *reinterpret_cast<u32x4 *>(ep.pre + row * ep.ldp + col) = C::narrow(v);
     if (ep.act != DASS_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = act_value<true>(v[i], ep.act);
+        for (int i = 0; i < N; ++i)
+            v[i] = act_value<FAST>(v[i], ep.act);
     }
     if (ep.mul) {
         C::widen(mul, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
             v[i] *= w[i];
     }
     if (ep.residual) {
         C::widen(residual, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
             v[i] += w[i];
     }
     *reinterpret_cast<u32x4 *>(ep.out + row * ep.ldo + col) = C::narrow(v);
 }
 
-template <Product PRODUCT, int RB, int CB>
-__global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16_t> a, const Epilogue<uint16_t> ep0, const TileOrder order)
+template <typename T_, Product PRODUCT, int RB, int CB>
+__global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a, const Epilogue<T_> ep0, const TileOrder order, const Split split)
 {
-    typedef Part<PRODUCT != kWeightGrad, RB, PRODUCT != kForward> PartP;
-    typedef Part<PRODUCT == kForward, CB, PRODUCT != kForward> PartQ;
+    constexpr bool BY_HAND = sizeof(T_) == 2 && PRODUCT != kForward;   // transposing reads
+    typedef Part<T_, PRODUCT != kWeightGrad, RB, BY_HAND> PartP;
+    typedef Part<T_, PRODUCT == kForward, CB, BY_HAND> PartQ;
+    constexpr int SLAB = kSlabBytes / sizeof(T_);
     constexpr int BR = 32 * RB, BC = 32 * CB;
     constexpr int NP = RB == 8 ? 3 : CB == 8 ? 4 : 5, NQ = RB == 8 ? 2 : CB == 8 ? 3 : 5, LEAD = NP - NQ;
     static_assert(NP * PartP::UNIT + NQ * PartQ::UNIT <= kLds && (LEAD == 0 || LEAD == 1), "the rings fit");
@@ -272,8 +337,13 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
         for (int j = 0; j < RB; ++j)
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int S = (int)((depth + kSlab - 1) / kSlab);
-    if (PRODUCT != kWeightGrad || S > 0) {
+    if (split.n > 1) {   // this workgroup's share of the slabs, perhaps none
+        const int64_t share = ((depth + SLAB - 1) / SLAB + split.n - 1) / split.n * SLAB, from = share * blockIdx.z;
+        depth = from >= depth ? 0 : depth - from < share ? depth - from : share;
+        k0 += from;
+    }
+    const int S = (int)((depth + SLAB - 1) / SLAB);
+    if (S > 0) {
     PartP P;
     PartQ Q;
     P.init(a.P, a.ldp, r0, r_end, k0, depth, wave, lane, wr);
@@ -365,7 +435,7 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
     // Instruction n of a K step: every one shares an operand with the one before.
     auto multiply = [&](const Frags &f, auto n) __attribute__((always_inline)) {
         constexpr int JP = decltype(n)::value / (2 * CB), X = decltype(n)::value % (2 * CB), I = X / 2, J = 2 * JP + ((X & 1) ^ (I & 1));
-        acc[I][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.q.get(I), f.p.get(J), acc[I][J], 0, 0, 0);
+        acc[I][J] = multiply_add(f.q.get(I), f.p.get(J), acc[I][J], T_{});
     };
 
     Frags f0, f1;
@@ -460,26 +530,35 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
     static_assert(NP <= 5, "every number of slabs left has its body");
     }
 
-    // ---- epilogue.  A wavefront passes strips of 16 rows through LDS of its own, as f32, so that a lane finishes eight
-    // neighbouring columns and rows are read and written in whole 128-byte lines.  mul and residual are requested
+    // ---- epilogue.  A wavefront passes strips of 16 rows through LDS of its own, as f32, so that a lane finishes 16 bytes
+    // of neighbouring columns and rows are read and written in whole 128-byte lines.  mul and residual are requested
     // AHEAD strips before they are needed, the first while the last sums are still being finished.
-    Epilogue<uint16_t> ep = ep0;
-    if constexpr (PRODUCT == kWeightGrad)
-        ep.out += (int64_t)expert * a.out_stride;
-    constexpr int SROW = 16 * CB * 4 + 16, LANES = 2 * CB, ROWS = 64 / LANES;   // lanes of a row; rows of a read
-    constexpr int READS_16 = 16 / ROWS, AHEAD = 3;
+    constexpr int N_CHUNK = Chunk<T_>::N;
+    constexpr int SROW = 16 * CB * 4 + 16, LANES = 16 * CB / N_CHUNK, ROWS = 64 / LANES;   // lanes of a row; rows of a read
+    constexpr int READS_16 = 16 / ROWS, AHEAD = RB < 3 ? RB : 3;
+    static_assert(ROWS * LANES == 64 && 2 * 16 * SROW <= kLds / 4, "strips");
+    Epilogue<T_> ep = ep0;
     char *const strips = lds + wave * (kLds / 4);
     const int fr = lane & 15, g = lane >> 4;
-    const int64_t row0 = r0 + wr * 16 * RB + lane / LANES, col = c0 + wc * 16 * CB + lane % LANES * 8;
-    float bias[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    const int64_t row0 = r0 + wr * 16 * RB + lane / LANES, col = c0 + wc * 16 * CB + lane % LANES * N_CHUNK;
+    int64_t share = blockIdx.z * split.stride;   // where this share's sums begin
+    if constexpr (PRODUCT == kWeightGrad) {
+        ep.out += (int64_t)expert * a.out_stride;
+        share += (int64_t)expert * a.out_rows * ep.cols;
+    }
+    float bias[N_CHUNK];
+#pragma unroll
+    for (int i = 0; i < N_CHUNK; ++i)
+        bias[i] = 0.0f;
     u32x4 mul[AHEAD + 1][READS_16], residual[AHEAD + 1][READS_16];
+    const bool whole = split.n == 1;
     auto request = [&](auto j_tag) __attribute__((always_inline)) {
         constexpr int J = decltype(j_tag)::value;
         if constexpr (J < RB && PRODUCT == kForward) {
 #pragma unroll
             for (int t = 0; t < READS_16; ++t) {
                 const int64_t r = row0 + J * 16 + t * ROWS;
-                if (r < r_end && col < ep.cols) {
+                if (whole && r < r_end && col < ep.cols) {
                     if (ep.mul)
                         mul[J % (AHEAD + 1)][t] = *reinterpret_cast<const u32x4 *>(ep.mul + r * ep.ldm + col);
                     if (ep.residual)
@@ -489,8 +568,8 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
         }
     };
     for_each<0, AHEAD>(request);
-    if (PRODUCT == kForward && ep.bias && col < ep.cols)
-        Chunk<uint16_t>::widen(*reinterpret_cast<const u32x4 *>(ep.bias + (int64_t)expert * ep.cols + col), bias);
+    if (PRODUCT == kForward && whole && ep.bias && col < ep.cols)
+        Chunk<T_>::widen(*reinterpret_cast<const u32x4 *>(ep.bias + (int64_t)expert * ep.cols + col), bias);
     block_barrier();   // the rings are about to be used again
     for_each<0, RB>([&](auto j_tag) __attribute__((always_inline)) {
         constexpr int J = decltype(j_tag)::value;
@@ -503,15 +582,26 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int t = 0; t < READS_16; ++t) {
-            const char *at = strip + (t * ROWS + lane / LANES) * SROW + lane % LANES * 32;
-            const f32x4 lo = *reinterpret_cast<const f32x4 *>(at), hi = *reinterpret_cast<const f32x4 *>(at + 16);
-            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            const char *at = strip + (t * ROWS + lane / LANES) * SROW + lane % LANES * N_CHUNK * 4;
+            f32x4 part[N_CHUNK / 4];
+            float v[N_CHUNK];
+#pragma unroll
+            for (int i = 0; i < N_CHUNK; ++i) {
+                if (i % 4 == 0)
+                    part[i / 4] = *reinterpret_cast<const f32x4 *>(at + i * 4);
+                v[i] = part[i / 4][i % 4];
+            }
             const int64_t r = row0 + J * 16 + t * ROWS;
             if (r < r_end && col < ep.cols) {
-                if constexpr (PRODUCT == kForward)
-                    finish8(ep, r, col, bias, mul[J % (AHEAD + 1)][t], residual[J % (AHEAD + 1)][t], v);
-                else
-                    *reinterpret_cast<u32x4 *>(ep.out + r * ep.ldo + col) = Chunk<uint16_t>::narrow(v);
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < N_CHUNK / 4; ++i)
+                        *reinterpret_cast<f32x4 *>(split.partial + share + r * ep.cols + col + 4 * i) = part[i];
+                } else if constexpr (PRODUCT == kForward) {
+                    finish(ep, r, col, bias, mul[J % (AHEAD + 1)][t], residual[J % (AHEAD + 1)][t], v);
+                } else {
+                    *reinterpret_cast<u32x4 *>(ep.out + r * ep.ldo + col) = Chunk<T_>::narrow(v);
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -519,52 +609,104 @@ __global__ __launch_bounds__(256) void product_bf16_kernel(const Operands<uint16
     });
 }
 
+// The outputs of a product whose k was split: the shares' sums are added in their order and finished.  A thread owns 16
+// bytes of a row of the output, a workgroup 256 of them in 256 / lanes rows of one expert.
+template <typename T_, Product PRODUCT>
+__global__ __launch_bounds__(256) void join_kernel(const Operands<T_> a, const Epilogue<T_> ep, const Split split, uint32_t strips)
+{
+    constexpr int N = Chunk<T_>::N;
+    const uint32_t tile = blockIdx.x / strips, strip = blockIdx.x - tile * strips;
+    const int64_t col = ((int64_t)strip * 32 + threadIdx.x % 32) * N;
+    int expert = 0;
+    int64_t row, out_row;
+    bool in = col < ep.cols;
+    T_ *out = ep.out;
+    if constexpr (PRODUCT == kWeightGrad) {   // rows of all experts in a row
+        row = (int64_t)tile * 8 + threadIdx.x / 32;
+        in = in && row < a.out_rows * a.seg.n;
+        const int64_t e = row / a.out_rows;
+        out_row = row - e * a.out_rows;
+        out += e * a.out_stride;
+    } else {
+        Span r;
+        if (!rows_of_tile(a.seg, tile, 8, expert, r))
+            return;
+        row = out_row = r.lo + threadIdx.x / 32;
+        in = in && row < r.hi;
+    }
+    if (!in)
+        return;
+    u32x4 mul, residual;
+    float bias[N], v[N];
+    if constexpr (PRODUCT == kForward) {
+        if (ep.mul)
+            mul = *reinterpret_cast<const u32x4 *>(ep.mul + row * ep.ldm + col);
+        if (ep.residual)
+            residual = *reinterpret_cast<const u32x4 *>(ep.residual + row * ep.ldr + col);
+        if (ep.bias)
+            Chunk<T_>::widen(*reinterpret_cast<const u32x4 *>(ep.bias + (int64_t)expert * ep.cols + col), bias);
+    }
+    f32x4 sum[N / 4];
+    const float *p = split.partial + row * ep.cols + col;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+        sum[i] = *reinterpret_cast<const f32x4 *>(p + 4 * i);
+#pragma unroll 4
+    for (int z = 1; z < split.n; ++z) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            sum[i] += *reinterpret_cast<const f32x4 *>(p + z * split.stride + 4 * i);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = sum[i / 4][i % 4];
+    if constexpr (PRODUCT == kForward)
+        finish(ep, row, col, bias, mul, residual, v);
+    else
+        *reinterpret_cast<u32x4 *>(out + out_row * ep.ldo + col) = Chunk<T_>::narrow(v);
+}
+
 // ------------------------------------------------------------------ host side --
-template <Product PRODUCT, int RB, int CB>
-static dass_status launch_tile(const char *fn, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, bool q_cached, hipStream_t stream)
+template <typename T_, Product PRODUCT, int RB, int CB>
+static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, const Split &split, hipStream_t stream)
 {
     constexpr int BR = 32 * RB, BC = 32 * CB;
     const int64_t tiles_r = PRODUCT == kWeightGrad ? (a.out_rows + BR - 1) / BR : tile_numbers(a.seg, BR);
     const int64_t tiles_c = (ep.cols + BC - 1) / BC;
-    const TileOrder order = make_tile_order(tiles_r, tiles_c, q_cached, BR < BC ? 8 : kPatchT);
+    const int64_t q_bytes = (PRODUCT == kWeightGrad ? a.seg.rows : a.depth) * ep.cols * (int64_t)sizeof(T_);
+    const TileOrder order = make_tile_order(tiles_r, tiles_c, q_bytes <= (256LL << 20), BR < BC ? 8 : kPatchT);
     const unsigned experts = PRODUCT == kWeightGrad ? a.seg.n : 1;
-    if (order.blocks == 0 || (int64_t)order.blocks * 256 * experts > 0xffffffffLL)
+    if (order.blocks == 0 || (int64_t)order.blocks * 256 > 0xffffffffLL / experts / split.n)
         return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_bf16_kernel<PRODUCT, RB, CB>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_tile_kernel<T_, PRODUCT, RB, CB>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess)
         return fail(DASS_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", fn, kLds, hipGetErrorString(e));
-    hipLaunchKernelGGL((product_bf16_kernel<PRODUCT, RB, CB>), dim3(order.blocks, experts), dim3(256), kLds, stream, a, ep, order);
-    return check_launch("bf16 product kernel");
+    hipLaunchKernelGGL((product_tile_kernel<T_, PRODUCT, RB, CB>), dim3(order.blocks, experts, split.n), dim3(256), kLds, stream, a, ep,
+                       order, split);
+    dass_status s = check_launch("product kernel");
+    if (s != DASS_OK || split.n == 1)
+        return s;
+    constexpr int N = Chunk<T_>::N;
+    const int64_t strips = (ep.cols + 32 * N - 1) / (32 * N);
+    const int64_t rows = PRODUCT == kWeightGrad ? (a.out_rows * a.seg.n + 7) / 8 : tile_numbers(a.seg, 8);
+    if (rows > 0xffffffffLL / 256 / strips)
+        return fail(DASS_ERR_SHAPE, "%s: too many rows for one launch; split the rows", fn);
+    hipLaunchKernelGGL((join_kernel<T_, PRODUCT>), dim3((unsigned)(rows * strips)), dim3(256), 0, stream, a, ep, split, (uint32_t)strips);
+    return check_launch("join kernel");
 }
 
-template <Product PRODUCT>
-static dass_status launch_any(const char *fn, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, hipStream_t stream)
+template <typename T_, Product PRODUCT>
+static dass_status launch_plan(const char *fn, const Plan &plan, const Operands<T_> &a, const Epilogue<T_> &ep, const Split &split,
+                               hipStream_t stream)
 {
-    // 32-bit byte offsets inside a tile: 256 rows (by rows), 64 lines of k (k by k)
-    if (256 * a.ldp * 2 >= 0x7fffffffLL || 256 * a.ldq * 2 >= 0x7fffffffLL)
-        return fail(DASS_ERR_SHAPE, "%s: rows too long for the tile addressing", fn);
-    // each expert's tiles count as if its rows were an even share
-    const int64_t groups = PRODUCT == kWeightGrad ? 1 : a.seg.n;
-    const int64_t rows = PRODUCT == kWeightGrad ? a.out_rows : (a.seg.rows + groups - 1) / groups;
-    const TileShape shape = dense_tile_shape(rows, ep.cols * groups, false);
-    const int64_t q_bytes = (PRODUCT == kWeightGrad ? a.seg.rows : a.depth) * ep.cols * 2;
-    const bool cached = q_bytes <= (256LL << 20);
-    if (shape.which == 0)
-        return launch_tile<PRODUCT, 8, 8>(fn, a, ep, cached, stream);
-    if (shape.which == 1)
-        return launch_tile<PRODUCT, 4, 8>(fn, a, ep, cached, stream);
-    return launch_tile<PRODUCT, 4, 4>(fn, a, ep, cached, stream);
-}
-
-dass_status launch_product_bf16(const char *fn, Product product, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,
-                                hipStream_t stream)
-{
-    if (product == kForward)
-        return launch_any<kForward>(fn, a, ep, stream);
-    if (product == kInputGrad)
-        return launch_any<kInputGrad>(fn, a, ep, stream);
-    return launch_any<kWeightGrad>(fn, a, ep, stream);
+    if constexpr (sizeof(T_) == 2) {
+        if (plan.tile == 0)
+            return launch_tiles<T_, PRODUCT, 8, 8>(fn, a, ep, split, stream);
+        if (plan.tile == 1)
+            return launch_tiles<T_, PRODUCT, 4, 8>(fn, a, ep, split, stream);
+    }
+    return launch_tiles<T_, PRODUCT, 4, 4>(fn, a, ep, split, stream);
 }
 
 }  // namespace dass

@@ -61,11 +61,11 @@ def _linear(lib, **change):
     t = dict(X=A, T=8, ldx=64, W=A, ldw=64, expert_stride=0, d_in=64, d_out=64, offsets=None, n_experts=1, bias=None, mul=None, ldm=0,
              residual=None, ldr=0, pre_out=None, ldp=0, out=A, ldo=64, dt=1, act=4)
     t.update(change)
-    return _name(lib, lib.dass_linear(ctypes.byref(binding.LinearTask(**t)), None))
+    return _name(lib, lib.dass_linear(ctypes.byref(binding.LinearTask(**t)), None, 0, None))
 
 
 def test_linear_rejections(lib):
-    assert _name(lib, lib.dass_linear(None, None)) == "NULL"
+    assert _name(lib, lib.dass_linear(None, None, 0, None)) == "NULL"
     for p, ld in (("X", "ldx"), ("W", "ldw"), ("out", "ldo")):
         assert _linear(lib, **{p: None}) == "NULL"
     for p, ld in (("X", "ldx"), ("W", "ldw"), ("out", "ldo"), ("mul", "ldm"), ("residual", "ldr"), ("pre_out", "ldp")):
