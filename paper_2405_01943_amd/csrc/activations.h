@@ -72,6 +72,35 @@ __device__ __forceinline__ float act_value(float x, int act)
     }
 }
 
+// act_value of N values at once: one decision for all of them.
+template <bool FAST, int N>
+__device__ __forceinline__ void act_values(float (&v)[N], int act)
+{
+    switch (act) {
+    case DASS_ACT_NONE:
+        break;
+    case DASS_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_value<FAST>(v[i], DASS_ACT_SILU);
+        break;
+    case DASS_ACT_GELU_TANH:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_value<FAST>(v[i], DASS_ACT_GELU_TANH);
+        break;
+    case DASS_ACT_GELU_ERF:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_value<FAST>(v[i], DASS_ACT_GELU_ERF);
+        break;
+    default:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_value<FAST>(v[i], DASS_ACT_RELU);
+    }
+}
+
 // act'(x):
 //   silu       s (1 + x (1 - s)),       s = 1 / (1 + exp(-x))
 //   gelu_tanh  s + x s (1 - s) z',      s = 1 / (1 + exp(-z)), z = 2 sqrt(2/pi) (x + 0.044715 x^3); x is held to
@@ -115,6 +144,38 @@ __device__ __forceinline__ float act_slope(float x, int act)
     }
     default:
         return x > 0.0f ? 1.0f : 0.0f;
+    }
+}
+
+// act_slope of N values at once.
+template <bool FAST, int N>
+__device__ __forceinline__ void act_slopes(const float (&x)[N], float (&v)[N], int act)
+{
+    switch (act) {
+    case DASS_ACT_NONE:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = 1.0f;
+        break;
+    case DASS_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_slope<FAST>(x[i], DASS_ACT_SILU);
+        break;
+    case DASS_ACT_GELU_TANH:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_slope<FAST>(x[i], DASS_ACT_GELU_TANH);
+        break;
+    case DASS_ACT_GELU_ERF:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_slope<FAST>(x[i], DASS_ACT_GELU_ERF);
+        break;
+    default:
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = act_slope<FAST>(x[i], DASS_ACT_RELU);
     }
 }
 

@@ -110,11 +110,9 @@ __device__ __forceinline__ void finish4(const Epilogue<T_> &ep, int expert, int6
         v += load4(ep.bias + (int64_t)expert * ep.cols + col);
     if (ep.pre)
         store4(ep.pre + row * ep.ldp + col, v);
-    if (ep.act != DASS_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = act_value<FAST>(v[i], ep.act);
-    }
+    float w[4] = {v[0], v[1], v[2], v[3]};
+    act_values<FAST>(w, ep.act);
+    v = f32x4{w[0], w[1], w[2], w[3]};
     if (ep.mul)
         v *= load4(ep.mul + row * ep.ldm + col);
     if (ep.residual)

@@ -50,7 +50,11 @@ __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout,
                 float y[N];
 #pragma unroll
                 for (int x = 0; x < N; ++x)
-                    y[x] = g[x] * act_value<FAST>(p[x], act);
+                    y[x] = p[x];
+                act_values<FAST>(y, act);
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    y[x] *= g[x];
                 *reinterpret_cast<u32x4 *>(dmul + row * lddm + c) = Chunk<T_>::narrow(y);
             }
             if (mul) {
@@ -59,9 +63,11 @@ __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout,
                     g[x] *= m[x];
             }
             if (act != DASS_ACT_NONE) {
+                float y[N];
+                act_slopes<FAST>(p, y, act);
 #pragma unroll
                 for (int x = 0; x < N; ++x)
-                    g[x] *= act_slope<FAST>(p[x], act);
+                    g[x] *= y[x];
             }
             if (g_out)
                 *reinterpret_cast<u32x4 *>(g_out + row * cols + c) = Chunk<T_>::narrow(g);

@@ -271,12 +271,8 @@ __device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int6
             v[i] += bias[i];
     }
     if (ep.pre)
-        *reinterpret_cast<u32x4 *>(ep.pre + row * ep.ldp + col) = C::narrow(v);
-    if (ep.act != DASS_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            v[i] = act_value<FAST>(v[i], ep.act);
-    }
+        __builtin_nontemporal_store(C::narrow(v), reinterpret_cast<u32x4 *>(ep.pre + row * ep.ldp + col));
+    act_values<FAST>(v, ep.act);
     if (ep.mul) {
         C::widen(mul, w);
 #pragma unroll
@@ -289,7 +285,7 @@ __device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int6
         for (int i = 0; i < N; ++i)
             v[i] += w[i];
     }
-    *reinterpret_cast<u32x4 *>(ep.out + row * ep.ldo + col) = C::narrow(v);
+    __builtin_nontemporal_store(C::narrow(v), reinterpret_cast<u32x4 *>(ep.out + row * ep.ldo + col));
 }
 
 template <typename T_, Product PRODUCT, int RB, int CB>
@@ -531,76 +527,86 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     }
 
     // ---- epilogue.  A wavefront passes strips of 16 rows through LDS of its own, as f32, so that a lane finishes 16 bytes
-    // of neighbouring columns and rows are read and written in whole 128-byte lines.  mul and residual are requested
-    // AHEAD strips before they are needed, the first while the last sums are still being finished.
+    // of neighbouring columns and rows are read and written in whole 128-byte lines.  Up to four strips lie there at a time,
+    // and a loop that is not unrolled goes over them: all of it unrolled, with five activations, was 200 KB of code that each tile
+    // fetched anew (4096 rows of 512 x 4096 37 us).  mul and residual are requested a strip ahead.
     constexpr int N_CHUNK = Chunk<T_>::N;
     constexpr int SROW = 16 * CB * 4 + 16, LANES = 16 * CB / N_CHUNK, ROWS = 64 / LANES;   // lanes of a row; rows of a read
-    constexpr int READS_16 = 16 / ROWS, AHEAD = RB < 3 ? RB : 3;
-    static_assert(ROWS * LANES == 64 && 2 * 16 * SROW <= kLds / 4, "strips");
+    constexpr int READS_16 = 16 / ROWS, HELD = RB < 4 ? RB : 4;
+    static_assert(ROWS * LANES == 64 && HELD * 16 * SROW <= kLds / 4 && RB % HELD == 0, "strips");
     Epilogue<T_> ep = ep0;
     char *const strips = lds + wave * (kLds / 4);
     const int fr = lane & 15, g = lane >> 4;
-    const int64_t row0 = r0 + wr * 16 * RB + lane / LANES, col = c0 + wc * 16 * CB + lane % LANES * N_CHUNK;
+    int64_t row = r0 + wr * 16 * RB + lane / LANES;
+    const int64_t col = c0 + wc * 16 * CB + lane % LANES * N_CHUNK;
     int64_t share = blockIdx.z * split.stride;   // where this share's sums begin
     if constexpr (PRODUCT == kWeightGrad) {
         ep.out += (int64_t)expert * a.out_stride;
         share += (int64_t)expert * a.out_rows * ep.cols;
     }
+    const bool whole = split.n == 1;
     float bias[N_CHUNK];
 #pragma unroll
     for (int i = 0; i < N_CHUNK; ++i)
         bias[i] = 0.0f;
-    u32x4 mul[AHEAD + 1][READS_16], residual[AHEAD + 1][READS_16];
-    const bool whole = split.n == 1;
-    auto request = [&](auto j_tag) __attribute__((always_inline)) {
-        constexpr int J = decltype(j_tag)::value;
-        if constexpr (J < RB && PRODUCT == kForward) {
+    u32x4 mul[READS_16], residual[READS_16];
+    auto request = [&](int64_t first) __attribute__((always_inline)) {
+        if constexpr (PRODUCT == kForward) {
 #pragma unroll
             for (int t = 0; t < READS_16; ++t) {
-                const int64_t r = row0 + J * 16 + t * ROWS;
+                const int64_t r = first + t * ROWS;
                 if (whole && r < r_end && col < ep.cols) {
                     if (ep.mul)
-                        mul[J % (AHEAD + 1)][t] = *reinterpret_cast<const u32x4 *>(ep.mul + r * ep.ldm + col);
+                        mul[t] = *reinterpret_cast<const u32x4 *>(ep.mul + r * ep.ldm + col);
                     if (ep.residual)
-                        residual[J % (AHEAD + 1)][t] = *reinterpret_cast<const u32x4 *>(ep.residual + r * ep.ldr + col);
+                        residual[t] = *reinterpret_cast<const u32x4 *>(ep.residual + r * ep.ldr + col);
                 }
             }
         }
     };
-    for_each<0, AHEAD>(request);
+    request(row);
     if (PRODUCT == kForward && whole && ep.bias && col < ep.cols)
         Chunk<T_>::widen(*reinterpret_cast<const u32x4 *>(ep.bias + (int64_t)expert * ep.cols + col), bias);
     block_barrier();   // the rings are about to be used again
-    for_each<0, RB>([&](auto j_tag) __attribute__((always_inline)) {
-        constexpr int J = decltype(j_tag)::value;
-        char *const strip = strips + (J & 1) * 16 * SROW;
-        request(std::integral_constant<int, J + AHEAD>{});
+    for_each<0, RB / HELD>([&](auto phase) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < CB; ++i)
-            *reinterpret_cast<f32x4 *>(strip + fr * SROW + (i * 16 + 4 * g) * 4) = acc[i][J];
+        for (int j = 0; j < HELD; ++j)
+#pragma unroll
+            for (int i = 0; i < CB; ++i)
+                *reinterpret_cast<f32x4 *>(strips + (j * 16 + fr) * SROW + (i * 16 + 4 * g) * 4) = acc[i][decltype(phase)::value * HELD + j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int j = 0; j < HELD; ++j, row += 16) {
+            u32x4 mul_now[READS_16], residual_now[READS_16];
 #pragma unroll
-        for (int t = 0; t < READS_16; ++t) {
-            const char *at = strip + (t * ROWS + lane / LANES) * SROW + lane % LANES * N_CHUNK * 4;
-            f32x4 part[N_CHUNK / 4];
-            float v[N_CHUNK];
-#pragma unroll
-            for (int i = 0; i < N_CHUNK; ++i) {
-                if (i % 4 == 0)
-                    part[i / 4] = *reinterpret_cast<const f32x4 *>(at + i * 4);
-                v[i] = part[i / 4][i % 4];
+            for (int t = 0; t < READS_16; ++t) {
+                mul_now[t] = mul[t];
+                residual_now[t] = residual[t];
             }
-            const int64_t r = row0 + J * 16 + t * ROWS;
-            if (r < r_end && col < ep.cols) {
-                if (!whole) {
+            request(row + 16);
 #pragma unroll
-                    for (int i = 0; i < N_CHUNK / 4; ++i)
-                        *reinterpret_cast<f32x4 *>(split.partial + share + r * ep.cols + col + 4 * i) = part[i];
-                } else if constexpr (PRODUCT == kForward) {
-                    finish(ep, r, col, bias, mul[J % (AHEAD + 1)][t], residual[J % (AHEAD + 1)][t], v);
-                } else {
-                    *reinterpret_cast<u32x4 *>(ep.out + r * ep.ldo + col) = Chunk<T_>::narrow(v);
+            for (int t = 0; t < READS_16; ++t) {
+                const char *at = strips + (j * 16 + t * ROWS + lane / LANES) * SROW + lane % LANES * N_CHUNK * 4;
+                f32x4 part[N_CHUNK / 4];
+                float v[N_CHUNK];
+#pragma unroll
+                for (int i = 0; i < N_CHUNK; ++i) {
+                    if (i % 4 == 0)
+                        part[i / 4] = *reinterpret_cast<const f32x4 *>(at + i * 4);
+                    v[i] = part[i / 4][i % 4];
+                }
+                const int64_t r = row + t * ROWS;
+                if (r < r_end && col < ep.cols) {
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < N_CHUNK / 4; ++i)
+                            *reinterpret_cast<f32x4 *>(split.partial + share + r * ep.cols + col + 4 * i) = part[i];
+                    } else if constexpr (PRODUCT == kForward) {
+                        finish(ep, r, col, bias, mul_now[t], residual_now[t], v);
+                    } else {
+                        __builtin_nontemporal_store(Chunk<T_>::narrow(v), reinterpret_cast<u32x4 *>(ep.out + r * ep.ldo + col));
+                    }
                 }
             }
         }
