@@ -479,23 +479,24 @@ def down_proj_sparse24(Y: torch.Tensor, values: torch.Tensor, meta: torch.Tensor
 _I32 = torch.int32
 
 
-def _on_device(stream, *tensors) -> None:
-    """Every tensor of a call is on the GPU whose stream it is enqueued on."""
+def _on_device(stream, *tensors) -> int:
+    """The handle of the stream that a call goes to; every tensor must be on that stream's GPU."""
     device = None
     for t in tensors:
-        if t is None:
-            continue
-        where = t.get_device()
-        if where < 0:
-            raise ValueError("every tensor must be on the GPU")
-        if device is None:
-            device = torch.cuda.current_device() if stream is None else stream.device_index
-        if where != device:
-            raise ValueError(f"a tensor on GPU {where}, the stream of GPU {device}")
+        if t is not None:
+            where = t.get_device()
+            if where != device:
+                if device is not None or where < 0:
+                    raise ValueError("every tensor must be on the GPU" if where < 0 else f"tensors on GPUs {device} and {where}")
+                device = where
+    current = torch.cuda.current_device() if stream is None else stream.device_index
+    if current != device:
+        raise ValueError(f"the tensors are on GPU {device}, the stream is of GPU {current}")
+    return _raw_stream(current) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _integers(t: torch.Tensor, name: str, shape) -> None:
-    if t.dtype != _I32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != _I32 or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name}: need contiguous int32 {tuple(shape)}")
 
 
@@ -516,13 +517,13 @@ def expert_sort(experts: torch.Tensor, n_experts: int, offsets: torch.Tensor, or
     _integers(offsets, "offsets", (n_experts + 1,))
     _integers(order, "order", (T * k,))
     _integers(place, "place", (T, k))
-    _on_device(stream, experts, offsets, order, place, workspace)
+    handle = _on_device(stream, experts, offsets, order, place, workspace)
     if workspace is None:
         need = int(lib.dass_expert_sort_workspace_bytes(T, k, n_experts))
         if need > 0:
             workspace = _scratch(need, experts.device, stream)
     status = lib.dass_expert_sort(_ptr(experts), experts.element_size(), T, k, n_experts, _ptr(offsets), _ptr(order),
-                                  _ptr(place), _ptr(workspace), _nbytes(workspace), _stream(stream))
+                                  _ptr(place), _ptr(workspace), _nbytes(workspace), handle)
     if status:
         _check(status)
 
@@ -541,8 +542,8 @@ def expert_gather(X: torch.Tensor, place: torch.Tensor, out: torch.Tensor, strea
     k = place.shape[-1]
     _integers(place, "place", (T, k))
     ldo = _rows_of_pairs(out, "out", T * k, d, X.dtype)
-    _on_device(stream, X, place, out)
-    status = lib.dass_expert_gather(_ptr(X), T, ldx, d, DTYPE[X.dtype], _ptr(place), k, _ptr(out), ldo, _stream(stream))
+    handle = _on_device(stream, X, place, out)
+    status = lib.dass_expert_gather(_ptr(X), T, ldx, d, DTYPE[X.dtype], _ptr(place), k, _ptr(out), ldo, handle)
     if status:
         _check(status)
 
@@ -561,9 +562,9 @@ def expert_combine(Y: torch.Tensor, place: torch.Tensor, out: torch.Tensor, weig
     ldr = 0 if residual is None else _rows_of_pairs(residual, "residual", T, d, out.dtype)
     if weights is not None and (weights.dtype != _F32 or weights.shape != place.shape or not weights.is_contiguous()):
         raise TypeError("weights: need contiguous float32 [T, k]")
-    _on_device(stream, Y, place, out, weights, residual)
+    handle = _on_device(stream, Y, place, out, weights, residual)
     status = lib.dass_expert_combine(_ptr(Y), ldy, _ptr(place), T, k, _ptr(weights), _ptr(residual), ldr, d, DTYPE[out.dtype],
-                                     _ptr(out), ldo, _stream(stream))
+                                     _ptr(out), ldo, handle)
     if status:
         _check(status)
 
@@ -580,9 +581,9 @@ def expert_combine_backward(dout: torch.Tensor, Y: torch.Tensor, place: torch.Te
     for name, t in (("weights", weights), ("dweights", dweights)):
         if t.dtype != _F32 or t.shape != place.shape or not t.is_contiguous():
             raise TypeError(f"{name}: need contiguous float32 [T, k]")
-    _on_device(stream, dout, Y, place, weights, dY, dweights)
+    handle = _on_device(stream, dout, Y, place, weights, dY, dweights)
     status = lib.dass_expert_combine_backward(_ptr(dout), ldg, _ptr(Y), ldy, _ptr(place), T, k, _ptr(weights), d,
-                                              DTYPE[dout.dtype], _ptr(dY), lddy, _ptr(dweights), _stream(stream))
+                                              DTYPE[dout.dtype], _ptr(dY), lddy, _ptr(dweights), handle)
     if status:
         _check(status)
 
@@ -647,14 +648,14 @@ def linear(X: torch.Tensor, W: torch.Tensor, out: torch.Tensor, act: str = "none
     ldm, ldr = _like(mul, "mul", shape, dt), _like(residual, "residual", shape, dt)
     ldp, ldo = _like(pre_out, "pre_out", shape, dt), _like(out, "out", shape, dt)
     _bias(bias, "bias", E, d_out, dt)
-    _on_device(stream, X, W, out, bias, mul, residual, pre_out, offsets, workspace)
+    handle = _on_device(stream, X, W, out, bias, mul, residual, pre_out, offsets, workspace)
     if workspace is None:
         need = int(lib.dass_linear_workspace_bytes(T, d_in, d_out, DTYPE[dt], max(E, 1)))
         if need > 0:
             workspace = _scratch(need, X.device, stream)
     task = LinearTask(_ptr(X), T, ldx, _ptr(W), ldw, per_expert, d_in, d_out, _ptr(offsets), max(E, 1), _ptr(bias), _ptr(mul),
                       ldm, _ptr(residual), ldr, _ptr(pre_out), ldp, _ptr(out), ldo, DTYPE[dt], code)
-    status = lib.dass_linear(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    status = lib.dass_linear(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), handle)
     if status:
         _check(status)
 
@@ -687,13 +688,13 @@ def linear_backward(dout: torch.Tensor, X: Optional[torch.Tensor], W: torch.Tens
     ldx, lddx = _like(X, "X", narrow, dt), _like(dX, "dX", narrow, dt)
     ldp, ldm, lddm = _like(pre, "pre", wide, dt), _like(mul, "mul", wide, dt), _like(dmul, "dmul", wide, dt)
     _bias(dbias, "dbias", E, d_out, dt)
-    _on_device(stream, dout, X, W, pre, mul, dX, dW, dbias, dmul, offsets, workspace)
+    handle = _on_device(stream, dout, X, W, pre, mul, dX, dW, dbias, dmul, offsets, workspace)
     if workspace is None:
         need = int(lib.dass_linear_backward_workspace_bytes(T, d_in, d_out, DTYPE[dt], max(E, 1)))
         workspace = _scratch(need, dout.device, stream)
     task = LinearGradTask(_ptr(dout), T, ldg, _ptr(X), ldx, _ptr(W), ldw, per_expert, d_in, d_out, _ptr(offsets), max(E, 1),
                           _ptr(pre), ldp, _ptr(mul), ldm, _ptr(dX), lddx, _ptr(dW), lddw, dw_per, _ptr(dbias), _ptr(dmul), lddm,
                           DTYPE[dt], code)
-    status = lib.dass_linear_backward(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    status = lib.dass_linear_backward(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), handle)
     if status:
         _check(status)

@@ -85,7 +85,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const ID *__re
     const int64_t lo = (int64_t)blockIdx.x * per_block, end = lo + per_block < pairs ? lo + per_block : pairs;
     const int64_t per_wave = per_block / kSortWaves, w_lo = lo + wave * per_wave;   // a multiple of 64
     const int64_t w_end = w_lo + per_wave < end ? w_lo + per_wave : end;
-    for (int64_t i = w_lo + lane; i < w_end; i += 64) {
+    // the experts of the first HELD pairs of each lane stay in registers for the second pass
+    constexpr int HELD = 8;
+    int held[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        held[h] = expert_of(ids, w_lo + h * 64 + lane, w_end, E);
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        if (w_lo + h * 64 + lane < w_end)
+            atomicAdd(&counts[wave * stride + (held[h] < E ? held[h] : E)], 1);
+    for (int64_t i = w_lo + HELD * 64 + lane; i < w_end; i += 64) {
         const int e = expert_of(ids, i, w_end, E);
         atomicAdd(&counts[wave * stride + (e < E ? e : E)], 1);
     }
@@ -143,14 +153,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const ID *__re
     __syncthreads();
 
     int32_t *mine = counts + wave * stride;
-    for (int64_t i = w_lo + lane; i - lane < w_end; i += 64) {
-        const int e = expert_of(ids, i, w_end, E);
+    auto place_64 = [&](int64_t i, int e) __attribute__((always_inline)) {
         const uint64_t same = same_expert(e, bits);
         int row = -1;
-        if (e < kMaxExperts) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            row = mine[e] + rank;
-        }
+        if (e < kMaxExperts)
+            row = mine[e] + __popcll(same & ((1ull << lane) - 1));
         wave_fence();
         if (e < kMaxExperts && (same >> lane) == 1)   // the highest lane of its expert
             mine[e] = row + 1;
@@ -160,7 +167,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const ID *__re
             if (row >= 0)
                 order[row] = (int32_t)i;
         }
-    }
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        if (w_lo + h * 64 < w_end)
+            place_64(w_lo + h * 64 + lane, held[h]);
+    for (int64_t i = w_lo + HELD * 64 + lane; i - lane < w_end; i += 64)
+        place_64(i, expert_of(ids, i, w_end, E));
     for (int64_t p = kept + (int64_t)blockIdx.x * kSortThreads + tid; p < pairs; p += (int64_t)gridDim.x * kSortThreads)
         order[p] = -1;
 }

@@ -66,6 +66,58 @@ inline int64_t tile_numbers(const Segments &s, int64_t bm)
     return s.offsets ? s.rows / bm + s.n : (s.rows + bm - 1) / bm;
 }
 
+// The same tiles in a row, without the numbers that hold none: their count and the rows of the tile-th, by a scan over the
+// experts.  For kernels that place tiles by their position in the list: tiles that are none, most of them with the smallest experts, left
+// some XCDs with an eighth less to do than others.
+struct TileList {
+    int total, scan;   // scan: tiles of the first 64 experts up to and with this lane's
+
+    static __device__ __forceinline__ int scan_64(const Segments &s, int e0, int bm, int &tiles)
+    {
+        const int lane = threadIdx.x & 63, e = e0 + lane;
+        tiles = 0;
+        if (e < s.n) {
+            const Span r = segment(s, e);
+            tiles = (int)((r.hi - r.lo + bm - 1) / bm);
+        }
+        int sum = tiles;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const int up = __shfl_up(sum, step, 64);
+            sum += lane >= step ? up : 0;
+        }
+        return sum;
+    }
+    __device__ __forceinline__ TileList(const Segments &s, int bm)
+    {
+        int tiles;
+        scan = scan_64(s, 0, bm, tiles);
+        total = __builtin_amdgcn_readlane(scan, 63);
+        for (int e0 = 64; e0 < s.n; e0 += 64)
+            total += __builtin_amdgcn_readlane(scan_64(s, e0, bm, tiles), 63);
+    }
+    // `tile` below total
+    __device__ __forceinline__ Span rows(const Segments &s, int bm, int tile, int &expert) const
+    {
+        int before = 0, e0 = 0, sum = scan, tiles;
+        for (;;) {
+            const int last = before + __builtin_amdgcn_readlane(sum, 63);
+            if (tile < last || e0 + 64 >= s.n)
+                break;
+            before = last;
+            e0 += 64;
+            sum = scan_64(s, e0, bm, tiles);
+        }
+        const int below = __popcll(__ballot(before + sum <= tile));
+        expert = e0 + below;
+        if (below > 0)
+            before += __builtin_amdgcn_readlane(sum, below - 1);
+        Span r = segment(s, expert);
+        r.lo += (int64_t)(tile - before) * bm;
+        return r;
+    }
+};
+
 // out = act(sum + bias) * mul + residual, pre = sum + bias.  Absent parts are nullptr.  All strides in elements.
 template <typename T_>
 struct Epilogue {

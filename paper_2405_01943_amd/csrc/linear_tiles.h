@@ -288,6 +288,18 @@ __device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int6
     __builtin_nontemporal_store(C::narrow(v), reinterpret_cast<u32x4 *>(ep.out + row * ep.ldo + col));
 }
 
+// Every XCD one contiguous run of the tiles, as tile_order.h has them, for a number of row tiles that only the device knows.
+__device__ __forceinline__ TileOrder order_runs(uint32_t tiles_r, uint32_t tiles_c, uint32_t max_band)
+{
+    const uint32_t bands = (tiles_r + max_band - 1) / max_band;
+    TileOrder o = {};
+    o.tiles_t = tiles_r;
+    o.tiles_n = tiles_c;
+    o.band = tiles_r > 0 ? (tiles_r + bands - 1) / bands : 1;
+    o.per_xcd = (tiles_r * tiles_c + kXcds - 1) / kXcds;
+    return o;
+}
+
 template <typename T_, Product PRODUCT, int RB, int CB>
 __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a, const Epilogue<T_> ep0, const TileOrder order, const Split split)
 {
@@ -303,21 +315,25 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     extern __shared__ __attribute__((aligned(1024))) char lds[];   // kLds bytes
 
     uint32_t tile_r, tile_c;   // tile_order.h
-    if (!tile_of_block(order, blockIdx.x, tile_r, tile_c))
-        return;
-    int expert;
+    int expert = 0;
     int64_t r0, r_end, k0 = 0, depth = a.depth;
-    if constexpr (PRODUCT == kWeightGrad) {
-        expert = blockIdx.y;
-        const Span k = segment(a.seg, expert);
-        k0 = k.lo;
-        depth = k.hi - k.lo;
-        r0 = (int64_t)tile_r * BR;
-        r_end = a.out_rows;
-    } else {
-        Span r;
-        if (!rows_of_tile(a.seg, tile_r, BR, expert, r))
+    if (PRODUCT == kWeightGrad || !a.seg.offsets) {
+        if (!tile_of_block(order, blockIdx.x, tile_r, tile_c))
             return;
+        r0 = (int64_t)tile_r * BR;
+        r_end = PRODUCT == kWeightGrad ? a.out_rows : a.seg.rows;
+        if constexpr (PRODUCT == kWeightGrad) {
+            expert = blockIdx.y;
+            const Span k = segment(a.seg, expert);
+            k0 = k.lo;
+            depth = k.hi - k.lo;
+        }
+    } else {   // the order for the tiles that there are: runs
+        const TileList list(a.seg, BR);
+        const TileOrder runs = order_runs(list.total, order.tiles_n, BR < BC ? 8 : kPatchT);
+        if (list.total == 0 || blockIdx.x / kXcds >= runs.per_xcd || !tile_of_block(runs, blockIdx.x, tile_r, tile_c))
+            return;
+        const Span r = list.rows(a.seg, BR, (int)tile_r, expert);
         r0 = r.lo;
         r_end = r.hi;
     }
@@ -680,7 +696,12 @@ static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epi
     const int64_t tiles_r = PRODUCT == kWeightGrad ? (a.out_rows + BR - 1) / BR : tile_numbers(a.seg, BR);
     const int64_t tiles_c = (ep.cols + BC - 1) / BC;
     const int64_t q_bytes = (PRODUCT == kWeightGrad ? a.seg.rows : a.depth) * ep.cols * (int64_t)sizeof(T_);
-    const TileOrder order = make_tile_order(tiles_r, tiles_c, q_bytes <= (256LL << 20), BR < BC ? 8 : kPatchT);
+    TileOrder order = make_tile_order(tiles_r, tiles_c, q_bytes <= (256LL << 20), BR < BC ? 8 : kPatchT);
+    if (PRODUCT != kWeightGrad && a.seg.offsets) {   // the kernel orders the tiles that there are
+        const int64_t n = (tiles_r * tiles_c + kXcds - 1) / kXcds * kXcds;
+        order.blocks = n <= 0x7fffffffLL ? (unsigned)n : 0;
+        order.tiles_n = (unsigned)tiles_c;
+    }
     const unsigned experts = PRODUCT == kWeightGrad ? a.seg.n : 1;
     if (order.blocks == 0 || (int64_t)order.blocks * 256 > 0xffffffffLL / experts / split.n)
         return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
