@@ -415,8 +415,8 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  *   offsets  NULL (n_experts = 1) or [n_experts + 1] int32, n_experts 1 to 1024
  *   bias     NULL or [n_experts, d_out];  mul, residual NULL or [T, d_out]
  *   pre_out  NULL or [T, d_out]: pre, as the gradient needs it
- *   out      [T, d_out]; may be mul or residual itself (same stride), but no
- *            other operand
+ *   out      [T, d_out]; may be mul or residual itself (same stride); no other
+ *            overlap
  *   workspace  dass_linear_workspace_bytes() bytes, 16-byte aligned (0 and NULL
  *            where the outputs are many; else partial sums over shares of d_in)
  * All of dtype dt (bf16 or f32); sums and epilogue are f32, rounded once (pre
@@ -433,8 +433,9 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  * dmul is not asked for.  Outputs must not overlap inputs.  g is rounded to dt for the two products, and dbias
  * is summed before that; everything else is f32 and rounded once.  Sums have a fixed order: the same
  * bits on every run.
- *   workspace  dass_linear_backward_workspace_bytes() bytes, 16-byte aligned (g
- *            and partial sums)
+ *   workspace  dass_linear_backward_workspace_bytes() bytes, 16-byte aligned: g
+ *            and partial sums.  A call without activation and mul, or of fewer
+ *            gradients, needs less and takes less.
  */
 typedef struct {
     const void *X;

@@ -9,6 +9,7 @@
 #include "linear.h"
 
 #include <algorithm>
+#include <initializer_list>
 
 namespace dass {
 
@@ -165,6 +166,13 @@ struct Checker {
         else if (!aligned16(p) || ld % vec != 0)
             status = fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
     }
+    // an output that begins where something else of the call does
+    void apart(const char *name, const void *out, std::initializer_list<const void *> others)
+    {
+        for (const void *p : others)
+            if (status == DASS_OK && out && p == out)
+                status = fail(DASS_ERR_ARG, "%s: %s must not overlap another operand", fn, name);
+    }
     void vector(const char *name, const void *p)
     {
         if (status == DASS_OK && p && !aligned16(p))
@@ -318,19 +326,22 @@ static dass_status run_linear(const char *fn, const dass_linear_task &t, void *w
     return launch_product(fn, kForward, t.d_in, t.d_out, a, ep, workspace, stream);
 }
 
+// Whether g is a matrix of its own.
+static bool keeps_g(const dass_linear_grad_task &t) { return (t.act != DASS_ACT_NONE || t.mul) && (t.dX || t.dW); }
+
 template <typename T_>
 static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &t, char *workspace, hipStream_t stream)
 {
     constexpr int N = Chunk<T_>::N;
     const Segments seg = {t.offsets, t.T, (int)t.n_experts};
-    const bool own_g = (t.act != DASS_ACT_NONE || t.mul) && (t.dX || t.dW);
+    const bool own_g = keeps_g(t);
     const T_ *g = static_cast<const T_ *>(t.dout);
     int64_t ldg = t.ldg;
-    // the workspace: g, then the partial sums of the bias, whose place the split products take after them
-    char *const shares = workspace + kept_bytes(t.T, t.d_out, t.dt);
+    // the workspace: g if it is kept, then the partial sums of the bias, whose place the split products take after them
+    char *const shares = workspace + (own_g ? kept_bytes(t.T, t.d_out, t.dt) : 0);
     if (own_g || t.dbias || t.dmul) {
         T_ *kept = own_g ? reinterpret_cast<T_ *>(workspace) : nullptr;
-        float *partial = t.dbias ? reinterpret_cast<float *>(workspace + kept_bytes(t.T, t.d_out, t.dt)) : nullptr;
+        float *partial = t.dbias ? reinterpret_cast<float *>(shares) : nullptr;
         const int tile_rows = sum_tile_rows(t.T, t.d_out, t.dt);
         const int64_t numbers = tile_numbers(seg, tile_rows), strips = (t.d_out + 64 * N - 1) / (64 * N);
         if (numbers > 0xffffffffLL / 256 / strips)
@@ -418,6 +429,10 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
     c.matrix("out", t.out, t.ldo, t.d_out, true);
     c.vector("bias", t.bias);
     c.stride("W", t.expert_stride, t.ldw, t.d_in, t.d_out, t.n_experts);
+    c.apart("out", t.out, {t.X, t.W, t.bias, t.pre_out});
+    c.apart("pre_out", t.pre_out, {t.X, t.W, t.bias, t.mul, t.residual});
+    if ((t.out == t.mul && t.ldo != t.ldm) || (t.out == t.residual && t.ldo != t.ldr))
+        c.apart("out", t.out, {t.out});
     if (c.status != DASS_OK)
         return c.status;
     const size_t need = dass_linear_workspace_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts);
@@ -429,17 +444,23 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
     return t.dt == DASS_BF16 ? run_linear<uint16_t>(fn, t, workspace, stream) : run_linear<float>(fn, t, workspace, stream);
 }
 
+namespace dass {
+// What a backward call needs: g if it is kept, then the most of the bias sums and of the split products' shares.
+static size_t backward_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW, bool dbias)
+{
+    const size_t sums = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
+    const size_t x = dX ? split_bytes(kInputGrad, dt, T, d_in, d_out, n_experts) : 0;
+    const size_t w = dW ? split_bytes(kWeightGrad, dt, T, d_in, d_out, n_experts) : 0;
+    return (keeps_g ? kept_bytes(T, d_out, dt) : 0) + std::max(sums, std::max(x, w));
+}
+}  // namespace dass
+
 extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
     using namespace dass;
     if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL)
         return 0;
-    size_t shares = partial_bytes(T, d_out, n_experts, dt);
-    for (const Product p : {kInputGrad, kWeightGrad}) {
-        const size_t b = split_bytes(p, dt, T, d_in, d_out, n_experts);
-        shares = b > shares ? b : shares;
-    }
-    return kept_bytes(T, d_out, dt) + shares;
+    return backward_bytes(T, d_in, d_out, dt, n_experts, true, true, true, true);
 }
 
 extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, void *workspace, size_t workspace_bytes,
@@ -467,16 +488,25 @@ extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, v
     c.matrix("dW", t.dW, t.lddw, t.d_in, false);
     c.matrix("dmul", t.dmul, t.lddm, t.d_out, false);
     c.vector("dbias", t.dbias);
+    const void *const inputs[] = {t.dout, t.X, t.W, t.pre, t.mul};
+    void *const outputs[] = {t.dX, t.dW, t.dbias, t.dmul};
+    const char *const names[] = {"dX", "dW", "dbias", "dmul"};
+    for (int i = 0; i < 4; ++i) {
+        for (const void *p : inputs)
+            c.apart(names[i], outputs[i], {p});
+        for (int j = 0; j < i; ++j)
+            c.apart(names[i], outputs[i], {outputs[j]});
+    }
     if (t.dX)
         c.stride("W", t.expert_stride, t.ldw, t.d_in, t.d_out, t.n_experts);
     if (t.dW)
         c.stride("dW", t.dw_stride, t.lddw, t.d_in, t.d_out, t.n_experts);
     if (c.status != DASS_OK)
         return c.status;
-    const size_t need = dass_linear_backward_workspace_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts);
-    if (!workspace || workspace_bytes < need)
+    const size_t need = backward_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts, keeps_g(t), t.dX, t.dW, t.dbias);
+    if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(DASS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
-    if (!aligned16(workspace))
+    if (need > 0 && !aligned16(workspace))
         return fail(DASS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", fn);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char *ws = static_cast<char *>(workspace);

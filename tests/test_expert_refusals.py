@@ -8,6 +8,7 @@ import paper_2405_01943_amd as dass
 from paper_2405_01943_amd import binding
 
 A, ODD = 0x10000, 0x10004          # aligned and not, never dereferenced
+B, C, D = 0x200000, 0x400000, 0x600000
 
 
 @pytest.fixture(scope="module")
@@ -59,7 +60,7 @@ def test_row_rejections(lib):
 
 def _linear(lib, **change):
     t = dict(X=A, T=8, ldx=64, W=A, ldw=64, expert_stride=0, d_in=64, d_out=64, offsets=None, n_experts=1, bias=None, mul=None, ldm=0,
-             residual=None, ldr=0, pre_out=None, ldp=0, out=A, ldo=64, dt=1, act=4)
+             residual=None, ldr=0, pre_out=None, ldp=0, out=B, ldo=64, dt=1, act=4)
     t.update(change)
     return _name(lib, lib.dass_linear(ctypes.byref(binding.LinearTask(**t)), None, 0, None))
 
@@ -80,11 +81,20 @@ def test_linear_rejections(lib):
     assert _linear(lib, n_experts=2) == _linear(lib, offsets=A, n_experts=1025) == "SHAPE"
     assert _linear(lib, offsets=A, n_experts=2, expert_stride=63 * 64) == "SHAPE"
     assert _linear(lib, offsets=A, n_experts=2, expert_stride=64 * 64 + 4) == "ALIGN"
+    # outputs over operands; mul and residual alone may be out, with its stride
+    assert _linear(lib, out=A) == _linear(lib, pre_out=B, ldp=64) == _linear(lib, pre_out=A, ldp=64) == "ARG"
+    assert _linear(lib, pre_out=C, ldp=64, mul=C, ldm=64) == "ARG"
+    assert _linear(lib, residual=B, ldr=72) == _linear(lib, mul=B, ldm=72) == "ARG"
+    # few rows of many columns: k is split, and its shares need room
+    assert lib.dass_linear_workspace_bytes(64, 4096, 512, 1, 1) > 0
+    wide = dict(T=64, d_in=4096, ldx=4096, ldw=4096, d_out=512, ldo=512)
+    assert _linear(lib, **wide) == "WORKSPACE"
+    assert lib.dass_linear_workspace_bytes(0, 64, 64, 1, 1) == lib.dass_linear_workspace_bytes(8, 64, 64, 9, 1) == 0
 
 
 def _grad(lib, ws=A, wsb=1 << 30, **change):
     t = dict(dout=A, T=8, ldg=64, X=A, ldx=64, W=A, ldw=64, expert_stride=0, d_in=64, d_out=64, offsets=None, n_experts=1, pre=A, ldp=64,
-             mul=None, ldm=0, dX=A, lddx=64, dW=A, lddw=64, dw_stride=0, dbias=None, dmul=None, lddm=0, dt=1, act=0)
+             mul=None, ldm=0, dX=B, lddx=64, dW=C, lddw=64, dw_stride=0, dbias=None, dmul=None, lddm=0, dt=1, act=0)
     t.update(change)
     return _name(lib, lib.dass_linear_backward(ctypes.byref(binding.LinearGradTask(**t)), ws, wsb, None))
 
@@ -102,6 +112,9 @@ def test_linear_backward_rejections(lib):
     assert _grad(lib, dt=2) == _grad(lib, act=5) == "DTYPE"
     assert _grad(lib, offsets=A, n_experts=2, expert_stride=64 * 64, dw_stride=8) == "SHAPE"
     assert _grad(lib, ws=None) == _grad(lib, wsb=64) == "WORKSPACE" and _grad(lib, ws=ODD) == "ALIGN"
+    for out in ("dX", "dW", "dbias"):
+        assert _grad(lib, **{out: A}) == "ARG"
+    assert _grad(lib, dX=C) == _grad(lib, mul=D, ldm=64, dmul=D, lddm=64) == _grad(lib, mul=D, ldm=64, dmul=B, lddm=64) == "ARG"
     need = lib.dass_linear_backward_workspace_bytes
     assert need(0, 64, 64, 1, 1) == 0 and need(8, 64, 64, 7, 1) == 0 and need(8, 64, 64, 1, 2000) == 0
     assert need(1000, 64, 688, 1, 4) >= 1000 * 688 * 2 + 4 * 688

@@ -108,6 +108,29 @@ def test_linear_sizes(gpu_device, T, d_in, d_out, dtype):
     _check_forward(p, "silu", out, pre, dtype, f"{T} x {d_in} -> {d_out}")
 
 
+# Larger grids: together, and with SIZES, they take every kernel: in bf16 the tiles of 256 x 256, 128 x 256 and 128 x 128, k whole
+# and split (2 to 12 shares), in f32 the tiles and both sizes of blocks, for the product and both gradients
+LARGE = [("bf16", 4224, 136, 4104, 0), ("bf16", 4100, 2056, 2056, 0), ("bf16", 2050, 264, 2056, 0), ("bf16", 5000, 264, 8200, 0),
+         ("bf16", 8200, 520, 1032, 0), ("bf16", 4096, 1032, 4104, 0), ("bf16", 130, 4104, 1032, 0), ("bf16", 9000, 264, 4104, 5),
+         ("bf16", 9000, 4104, 264, 5), ("bf16", 12000, 136, 264, 3), ("bf16", 700, 2056, 264, 5), ("f32", 4100, 264, 1032, 0),
+         ("f32", 4100, 1032, 264, 0), ("f32", 9000, 132, 132, 0), ("f32", 9000, 132, 260, 3)]
+
+
+@pytest.mark.parametrize("dtype,T,d_in,d_out,E", LARGE)
+def test_linear_large(gpu_device, dtype, T, d_in, d_out, E):
+    p = _make(T, d_in, d_out, dtype, E=E, tail=31 if E else 0)
+    out, pre = _forward(p, "silu", dtype)
+    _check_forward(p, "silu", out, pre, dtype, f"{T} x {d_in} -> {d_out}")
+
+
+@pytest.mark.parametrize("dtype,T,d_in,d_out,E", LARGE)
+def test_linear_backward_large(gpu_device, dtype, T, d_in, d_out, E):
+    p = _make(T, d_in, d_out, dtype, E=E, tail=31 if E else 0)
+    pre, dout = _saved(p, dtype)
+    got = _backward(p, "silu", pre, dtype, dout=dout)
+    _check_backward(p, "silu", pre, dout, got, dtype, f"{T} x {d_in} -> {d_out}")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ref.ACTS)
 @pytest.mark.parametrize("bias,mul,residual,keep", [(0, 0, 0, 0), (1, 0, 0, 1), (0, 1, 0, 0), (0, 0, 1, 0), (1, 1, 1, 1)])
