@@ -377,7 +377,7 @@ dass_status dass_down_proj_sparse24(const void *Y, int64_t T, int64_t ldy, const
  *   residual is dout.
  *
  * X, out of the gather etc. are rows of d elements of dtype dt; d is a multiple
- * of 8 (bf16) or 4 (f32).  Entries of place outside 0 .. T k - 1 count as
+ * of 8 (bf16) or 4 (f32) up to 2^24.  Entries of place outside 0 .. T k - 1 count as
  * pairs that go nowhere.  place must not hold a row twice where rows are written.
  */
 size_t dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t n_experts);
@@ -420,7 +420,8 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  *   workspace  dass_linear_workspace_bytes() bytes, 16-byte aligned (0 and NULL
  *            where the outputs are many; else partial sums over shares of d_in)
  * All of dtype dt (bf16 or f32); sums and epilogue are f32, rounded once (pre
- * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32), T below 2^31.
+ * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32) up to 2^24,
+ * T is below 2^31, row strides are at most 2^36.
  *
  * dass_linear_backward gives, with g = dout * mul * act'(pre),
  *

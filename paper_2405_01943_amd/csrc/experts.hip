@@ -323,8 +323,8 @@ static dass_status check_rows(const char *fn, const char *name, const void *p, i
 {
     if (!p)
         return fail(DASS_ERR_NULL, "%s: %s must not be NULL", fn, name);
-    if (ld < d)
-        return fail(DASS_ERR_SHAPE, "%s: rows of %s: stride %lld < d=%lld", fn, name, (long long)ld, (long long)d);
+    if (ld < d || ld > 1LL << 36)
+        return fail(DASS_ERR_SHAPE, "%s: rows of %s: stride %lld < d=%lld or beyond 2^36", fn, name, (long long)ld, (long long)d);
     if (!aligned16(p) || ld % vec != 0)
         return fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
     return DASS_OK;
@@ -334,8 +334,8 @@ static dass_status check_row_length(const char *fn, int64_t d, dass_dtype dt)
 {
     if (!valid_dtype(dt))
         return fail(DASS_ERR_DTYPE, "%s: unknown dtype %d", fn, (int)dt);
-    if (d <= 0 || d % vec_elems(dt) != 0 || d > 0x7fffffffLL)
-        return fail(DASS_ERR_SHAPE, "%s: d=%lld must be a positive multiple of %d", fn, (long long)d, vec_elems(dt));
+    if (d <= 0 || d % vec_elems(dt) != 0 || d > 1 << 24)
+        return fail(DASS_ERR_SHAPE, "%s: d=%lld must be a positive multiple of %d, at most 2^24", fn, (long long)d, vec_elems(dt));
     return DASS_OK;
 }
 

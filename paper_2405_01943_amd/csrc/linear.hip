@@ -14,6 +14,7 @@
 namespace dass {
 
 constexpr int kMaxLinearExperts = 1024;
+constexpr int64_t kMaxWidth = 1 << 24, kMaxStride = 1LL << 36;   // every product of sizes stays within 64 bits
 
 // ------------------------------------------------------ element-wise gradient and sums --
 // A wavefront owns 64 chunks of 16 bytes of columns and every fourth row of a tile of rows of one expert.  One pass:
@@ -160,9 +161,9 @@ struct Checker {
             return;
         if (!p)
             status = fail(DASS_ERR_NULL, "%s: %s must not be NULL", fn, name);
-        else if (ld < width)
-            status = fail(DASS_ERR_SHAPE, "%s: row stride %lld of %s is shorter than its rows of %lld", fn, (long long)ld, name,
-                          (long long)width);
+        else if (ld < width || ld > kMaxStride)
+            status = fail(DASS_ERR_SHAPE, "%s: row stride %lld of %s is shorter than its rows of %lld or beyond 2^36", fn, (long long)ld,
+                          name, (long long)width);
         else if (!aligned16(p) || ld % vec != 0)
             status = fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
     }
@@ -187,8 +188,9 @@ struct Checker {
         else if (T <= 0 || d_in <= 0 || d_out <= 0)
             status = fail(DASS_ERR_SHAPE, "%s: T=%lld d_in=%lld d_out=%lld must be positive", fn, (long long)T, (long long)d_in,
                           (long long)d_out);
-        else if (T > 0x7fffffffLL)
-            status = fail(DASS_ERR_SHAPE, "%s: T=%lld rows do not fit an int32", fn, (long long)T);
+        else if (T > 0x7fffffffLL || d_in > kMaxWidth || d_out > kMaxWidth)
+            status = fail(DASS_ERR_SHAPE, "%s: T=%lld must be below 2^31, d_in=%lld and d_out=%lld at most 2^24", fn, (long long)T,
+                          (long long)d_in, (long long)d_out);
         else if (d_in % vec_elems(dt) != 0 || d_out % vec_elems(dt) != 0)
             status = fail(DASS_ERR_SHAPE, "%s: d_in=%lld and d_out=%lld must be multiples of %d", fn, (long long)d_in,
                           (long long)d_out, vec_elems(dt));
@@ -200,8 +202,9 @@ struct Checker {
     }
     void stride(const char *name, int64_t stride, int64_t ld, int64_t d_in, int64_t d_out, int64_t n_experts)
     {
-        if (status == DASS_OK && n_experts > 1 && stride < (d_out - 1) * ld + d_in)
-            status = fail(DASS_ERR_SHAPE, "%s: expert stride %lld of %s is shorter than a matrix", fn, (long long)stride, name);
+        if (status == DASS_OK && n_experts > 1 && (stride < (d_out - 1) * ld + d_in || stride > 1LL << 50))
+            status = fail(DASS_ERR_SHAPE, "%s: expert stride %lld of %s is shorter than a matrix or beyond 2^50", fn, (long long)stride,
+                          name);
         if (status == DASS_OK && n_experts > 1 && stride % vec != 0)
             status = fail(DASS_ERR_ALIGN, "%s: expert stride of %s must be a multiple of %d elements", fn, name, vec);
     }
@@ -219,18 +222,16 @@ struct Checker {
 //           256 x 256; dX of 6000 rows of 4096 x 11008 473 / 503 / -; 64 rows of 11008 x 4096 (128 x 128) 88 us, 27 with 8 shares; dW of 16384 rows of 512 x 512 145, 28
 //           with 8; one share where the tiles fill the chip: 2048 rows of 4096 x 4096 59 us, 86 with 2.
 //   few     (f32) a fixed part that grows with k, or the workgroups and their multiplications.  512 rows of 256 x 688: blocks
-//           of 16 / of 32 / tiles 14.5 / 8.1 / 16.6 us, 16 of 1024 x 1024 9.3 / 14.0 / 11.5, 2048 of 512 x 512 32 / 19 / 27,
+//           of 16 / of 32 / tiles 13.2 / 6.7 / 16.6 us, 16 of 1024 x 1024 5.7 / 8.9 / 11.5, 1024 of 512 x 512 17 / 10 / 19,
 //           4096 of 1024 x 1024 225 / 119 / 71.
-//           (bf16, forward only) up to 8 rows where 128 x 128 tiles leave compute units idle, and one row an expert: one row of
-//           4096 x 11008 19.5 us (tiles with 4 shares 24), 8 of it 22.9 (24), 16 of it 27 (24); 8 rows over 5 experts of 4096 x
-//           14336 98 (130), but 16 over 8 170 (163).
+//           (bf16, forward only) the weights' bytes, or one workgroup's.  Up to 8 rows: one row of 4096 x 11008 17.7 us (tiles
+//           with 4 shares 24), 8 of it 22.2 (24), 16 of it 27 (24); 16384 x 256 19.6 with 16 workgroups (tiles with 16
+//           shares 13.4).  One row an expert: 8 rows over 5 experts of 4096 x 14336 98 (130), but 16 over 8 170 (163).
 static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, int64_t cols, int64_t depth)
 {
     const bool bf16 = dt == DASS_BF16;
     const auto pieces = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
     const int64_t share = product == kWeightGrad ? rows : pieces(rows, groups);   // of an expert, were they even
-    if (bf16 && product == kForward && (share == 1 || (share <= 8 && groups * pieces(cols, 128) < 256)))
-        return {Plan::kFew, 0, 1, 1};
     // the row tiles of experts of uneven size: half a tile more each
     const auto row_tiles = [&](int64_t of) {
         if (product == kWeightGrad || groups == 1)
@@ -245,6 +246,7 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
     } kTiles[] = {{256, 256, 5.4, 1.0}, {128, 256, 3.3, 0.67}, {128, 128, 1.9, 0.435}}, kTileF32 = {128, 128, 3.4, 2.49};
     const double join = bf16 ? 4.4 : 2.4, byte = bf16 ? 1 / 6.9e6 : 1 / 4.5e6;   // us, us a byte
     const int64_t slabs = pieces(depth, bf16 ? 64 : 32), outputs = (product == kWeightGrad ? groups : 1) * rows * cols;
+    const double weights = product == kWeightGrad ? 0 : (bf16 ? 2.0 : 4.0) * groups * cols * depth / 4.6e6;   // out of memory
     Plan best = {Plan::kTiles, bf16 ? 0 : 2, 1, 0};
     double best_time = 1e300;
     for (int k = bf16 ? 0 : 2; k < 3; ++k) {
@@ -253,19 +255,26 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
         for (const int z : kShares) {
             if (z > 1 && (slabs < 2 * z || (double)z * outputs * 4 > 256e6))
                 break;
-            const double time = pieces(tiles * z, 256) * (t.start + pieces(slabs, z) * t.slab) + (z > 1 ? join + z * 8.0 * outputs * byte : 0);
+            const double busy = pieces(tiles * z, 256) * (t.start + pieces(slabs, z) * t.slab);
+            const double time = std::max(busy, weights) + (z > 1 ? join + z * 8.0 * outputs * byte : 0);
             if (time < best_time) {
                 best_time = time;
                 best = {Plan::kTiles, k, z, 0};
             }
         }
     }
+    if (bf16 && product == kForward && share <= 8) {
+        const double bytes = 2.0 * groups * cols * depth * (1 + 0.035 * (share - 1));
+        if ((share == 1 && groups > 1) || std::max(2 + 0.0011 * depth, bytes / 4.9e6) < best_time)
+            return {Plan::kFew, 0, 1, 1};
+    }
     for (int blocks = 1; !bf16 && blocks <= 2; ++blocks) {
-        const double groups_of_4 = (double)row_tiles(16 * blocks) * pieces(cols, 16 * blocks);
-        const double fixed = blocks == 1 ? 7 + 0.0022 * depth : 6.5 + 0.0075 * depth;
-        const double busy = 5 + groups_of_4 * (0.006 + (blocks == 1 ? 28e-9 : 20.7e-9) * 256 * blocks * blocks * depth);
+        const double workgroups = (double)row_tiles(16 * blocks) * pieces(cols, 16 * blocks);
+        const double products = workgroups * 256 * blocks * blocks * depth;
+        const double fixed = blocks == 1 ? 2.8 + 0.0028 * depth : 2.6 + 0.0065 * depth;
+        const double busy = blocks == 1 ? 2 + 0.0085 * workgroups + 23e-9 * products : 3 + 0.001 * workgroups + 27e-9 * products;
         if (fixed < best_time && busy < best_time) {
-            best_time = fixed > busy ? fixed : busy;
+            best_time = std::max(fixed, busy);
             best = {Plan::kFew, 0, 1, blocks};
         }
     }
@@ -407,7 +416,8 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
 extern "C" size_t dass_linear_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
     using namespace dass;
-    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL)
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL ||
+        d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
     return split_bytes(kForward, dt, T, d_in, d_out, n_experts);
 }
@@ -458,7 +468,8 @@ static size_t backward_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype 
 extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
     using namespace dass;
-    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL)
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL ||
+        d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
     return backward_bytes(T, d_in, d_out, dt, n_experts, true, true, true, true);
 }

@@ -156,26 +156,32 @@ static dass_status launch(const char *fn, const Operands<T_> &a, const Epilogue<
     return check_launch("few-tile product kernel");
 }
 
+// Wavefronts of a workgroup and loads that each has on its way, in graphs: one row of 4096 x 11008 4 wavefronts x 8 fragments 20.0 us, 8
+// x 4 19.1, 16 x 4 17.7; of 4096 x 4096 9.4, 8.8, 8.3; but of 1024 x 4096 4.0 (x 4 3.9), 4.0, 5.1, four rows of 512 x 512 3.4 (x 4
+// 2.8), 3.4, 3.6.
 dass_status launch_few(const char *fn, Product, const Plan &, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, hipStream_t stream)
 {
-    return launch<uint16_t, kForward, 1, 1, 4, 4>(fn, a, ep, stream);
+    if (a.depth >= 4096)
+        return launch<uint16_t, kForward, 1, 1, 16, 2>(fn, a, ep, stream);
+    return launch<uint16_t, kForward, 1, 1, 4, 2>(fn, a, ep, stream);
+}
+
+// The same in f32, 8 wavefronts against 4 with twice the loads: 16 rows of 1024 x 1024 5.7 and 6.9 us, 301 of 256 x 688 (blocks of 32) 4.7
+// and 5.2, its dX 7.7 and 9.1, dW 5.3 and 6.6.
+template <int BLOCKS>
+static dass_status launch_blocks(const char *fn, Product product, const Operands<float> &a, const Epilogue<float> &ep, hipStream_t stream)
+{
+    if (product == kForward)
+        return launch<float, kForward, BLOCKS, BLOCKS, 8, 2 / BLOCKS>(fn, a, ep, stream);
+    if (product == kInputGrad)
+        return launch<float, kInputGrad, BLOCKS, BLOCKS, 8, 2 / BLOCKS>(fn, a, ep, stream);
+    return launch<float, kWeightGrad, BLOCKS, BLOCKS, 8, 2 / BLOCKS>(fn, a, ep, stream);
 }
 
 dass_status launch_few(const char *fn, Product product, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep,
                        hipStream_t stream)
 {
-    if (plan.blocks == 1) {
-        if (product == kForward)
-            return launch<float, kForward, 1, 1, 4, 4>(fn, a, ep, stream);
-        if (product == kInputGrad)
-            return launch<float, kInputGrad, 1, 1, 4, 4>(fn, a, ep, stream);
-        return launch<float, kWeightGrad, 1, 1, 4, 4>(fn, a, ep, stream);
-    }
-    if (product == kForward)
-        return launch<float, kForward, 2, 2, 4, 2>(fn, a, ep, stream);
-    if (product == kInputGrad)
-        return launch<float, kInputGrad, 2, 2, 4, 2>(fn, a, ep, stream);
-    return launch<float, kWeightGrad, 2, 2, 4, 2>(fn, a, ep, stream);
+    return plan.blocks == 1 ? launch_blocks<1>(fn, product, a, ep, stream) : launch_blocks<2>(fn, product, a, ep, stream);
 }
 
 }  // namespace dass

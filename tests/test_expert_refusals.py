@@ -50,7 +50,7 @@ def test_row_rejections(lib):
     for call in (gather, combine, grad):
         assert call(X=None) == call(place=None) == call(out=None) == "NULL"
         assert call(dt=2) == "DTYPE"
-        assert call(T=0) == call(k=0) == call(k=65) == call(d=0) == call(d=60) == call(ldx=56) == call(ldo=56) == "SHAPE"
+        assert call(T=0) == call(k=0) == call(k=65) == call(d=0) == call(d=60) == call(ldx=56) == call(ldo=56) == call(ldx=2 ** 50) == "SHAPE"
         assert call(T=2 ** 30, k=2) == "SHAPE"
         assert call(X=ODD) == call(out=ODD) == call(ldx=68) == call(ldo=68) == call(place=0x10002) == "ALIGN"
     assert gather(T=1 << 24, d=1 << 20, ldx=1 << 20, ldo=1 << 20) == "SHAPE"      # more chunks than a launch has threads
@@ -77,6 +77,7 @@ def test_linear_rejections(lib):
     assert _linear(lib, dt=2) == _linear(lib, act=5) == _linear(lib, act=-1) == "DTYPE"
     for name in ("T", "d_in", "d_out", "n_experts"):
         assert _linear(lib, **{name: 0}) == "SHAPE"
+    assert _linear(lib, d_in=2 ** 25, ldx=2 ** 25, ldw=2 ** 25) == _linear(lib, ldx=2 ** 40) == _linear(lib, offsets=A, n_experts=2, expert_stride=2 ** 60) == "SHAPE"
     assert _linear(lib, T=2 ** 31) == _linear(lib, d_in=60) == _linear(lib, d_out=60) == "SHAPE"
     assert _linear(lib, n_experts=2) == _linear(lib, offsets=A, n_experts=1025) == "SHAPE"
     assert _linear(lib, offsets=A, n_experts=2, expert_stride=63 * 64) == "SHAPE"
