@@ -17,9 +17,9 @@
 //             bytes of line k lie in place piece ^ (k / 4 mod 4), so that the four lines of a read meet all banks once.
 // So no operand is transposed in memory: the three products (linear.h) differ in their operands' forms alone.
 //
-// LDS is two rings, NP parts of P and NQ of Q, as many as 160 KB hold.  The places of slab s are free after the one
+// LDS is two rings, ND parts of the operand that leads and NF of the one that follows, as many as 160 KB hold.  The places of slab s are free after the one
 // barrier of the slab, which stands where every wavefront has read its last fragments of it, in the middle of its second
-// K step; the loads of Q's slab s + NQ and P's slab s + NP are spread over the matrix instructions from there to the
+// K step; the loads of the follower's slab s + NF and the leader's s + ND are spread over the matrix instructions from there to the
 // next barrier.  The wait before a barrier counts the loads that may still be on their way, so their order is
 // pinned; only slabs that exist are requested, and the last slabs have bodies of their own with fewer to wait for.
 //
@@ -308,9 +308,14 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     typedef Part<T_, PRODUCT == kForward, CB, BY_HAND> PartQ;
     constexpr int SLAB = kSlabBytes / sizeof(T_);
     constexpr int BR = 32 * RB, BC = 32 * CB;
-    constexpr int NP = RB == 8 ? 3 : CB == 8 ? 4 : 5, NQ = RB == 8 ? 2 : CB == 8 ? 3 : 5, LEAD = NP - NQ;
+    // Ring parts of the operand that leads and of the one that follows.  The weights lead in the large tiles of dX: 6000 rows of 4096 x
+    // 11008 486 -> 475 us, over 8 experts 541 -> 533; in the forward product they do not (8192 rows of 4096 x 14336 690, with
+    // them 699; over 8 experts 880 and 867).
+    constexpr bool Q_LEADS = RB == 8 && PRODUCT == kInputGrad;
+    constexpr int ND = RB == 8 ? 3 : CB == 8 ? 4 : 5, NF = RB == 8 ? 2 : CB == 8 ? 3 : 5, LEAD = ND - NF;
+    constexpr int NP = Q_LEADS ? NF : ND, NQ = Q_LEADS ? ND : NF;
     static_assert(NP * PartP::UNIT + NQ * PartQ::UNIT <= kLds && (LEAD == 0 || LEAD == 1), "the rings fit");
-    constexpr int PL = PartP::LOADS, QL = PartQ::LOADS, NL = PL + QL;
+    constexpr int DL = Q_LEADS ? PartQ::LOADS : PartP::LOADS, FL = Q_LEADS ? PartP::LOADS : PartQ::LOADS, NL = DL + FL;
     constexpr int N = RB * CB;   // matrix instructions of a K step
     extern __shared__ __attribute__((aligned(1024))) char lds[];   // kLds bytes
 
@@ -362,7 +367,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     Q.init(PRODUCT == kWeightGrad ? a.Q : a.Q + (int64_t)expert * a.q_stride, a.ldq, c0, ep0.cols, k0, depth, wave, lane, wc);
     char *const p_ring = lds, *const q_ring = lds + NP * PartP::UNIT;
 
-    // ---- the loads.  Iteration t (after the barrier of slab t) requests Q's slab t + NQ, then P's slab t + NP.
+    // ---- the loads.  Iteration t (after the barrier of slab t) requests the follower's slab t + NF, then the leader's t + ND.
     auto load_p = [&](int unit, int slab, int q, auto last) __attribute__((always_inline)) {
         P.template load<decltype(last)::value>(p_ring + unit * PartP::UNIT, wave, slab, q);
         __builtin_amdgcn_sched_barrier(0);
@@ -371,33 +376,47 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
         Q.template load<decltype(last)::value>(q_ring + unit * PartQ::UNIT, wave, slab, q);
         __builtin_amdgcn_sched_barrier(0);
     };
-    constexpr int AT_ONCE = (NL + 3) / 4;   // of an iteration's loads, those right after its barrier
-    static_assert(AT_ONCE <= QL, "they are Q's");
-    auto all_p = [&](int slab) {
-        if (slab < S) {
+    auto load = [&](auto leader, int unit, int slab, int q, auto last) __attribute__((always_inline)) {
+        if constexpr (decltype(leader)::value == Q_LEADS)
+            load_q(unit, slab, q, last);
+        else
+            load_p(unit, slab, q, last);
+    };
+    auto begin_slab = [&](auto leader, int slab) __attribute__((always_inline)) {
+        if constexpr (decltype(leader)::value == Q_LEADS)
+            Q.begin_slab(slab);
+        else
             P.begin_slab(slab);
+    };
+    constexpr std::true_type LEADER{};
+    constexpr std::false_type FOLLOWER{};
+    constexpr int AT_ONCE = (NL + 3) / 4;   // of an iteration's loads, those right after its barrier
+    static_assert(AT_ONCE <= FL, "they are the follower's");
+    auto whole_leader = [&](int slab) {
+        if (slab < S) {
+            begin_slab(LEADER, slab);
 #pragma unroll
-            for (int q = 0; q < PL; ++q)
-                load_p(slab % NP, slab, q, std::true_type{});
+            for (int q = 0; q < DL; ++q)
+                load(LEADER, slab % ND, slab, q, std::true_type{});
         }
     };
     if (LEAD == 1)
-        all_p(0);
+        whole_leader(0);
 #pragma unroll
-    for (int t = -NQ; t < -1; ++t) {
-        if (t + NQ < S) {
-            Q.begin_slab(t + NQ);
+    for (int t = -NF; t < -1; ++t) {
+        if (t + NF < S) {
+            begin_slab(FOLLOWER, t + NF);
 #pragma unroll
-            for (int q = 0; q < QL; ++q)
-                load_q(t + NQ, t + NQ, q, std::true_type{});
+            for (int q = 0; q < FL; ++q)
+                load(FOLLOWER, t + NF, t + NF, q, std::true_type{});
         }
-        all_p(t + NP);
+        whole_leader(t + ND);
     }
-    if (NQ - 1 < S) {
-        Q.begin_slab(NQ - 1);
+    if (NF - 1 < S) {
+        begin_slab(FOLLOWER, NF - 1);
 #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q)
-            load_q(NQ - 1, NQ - 1, q, std::true_type{});
+            load(FOLLOWER, NF - 1, NF - 1, q, std::true_type{});
     }
     // The sums stay in accumulation registers: cleared while the loads are on their way, and held there between slabs (left to
     // itself the compiler moves some to and fro, or spills in the first slab).
@@ -409,20 +428,20 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
                 asm volatile("" : "+a"(acc[i][j]));
     };
     pin();
-    // slab 0 has landed: all but the first part of P and of Q may be on their way
+    // slab 0 has landed: all but the first parts may be on their way
     auto begin = [&](auto slabs_tag) __attribute__((always_inline)) {
-        constexpr int HAVE = decltype(slabs_tag)::value;   // slabs, at most NP
-        constexpr int P_OUT = (HAVE < NP - 1 ? HAVE : NP - 1) - 1, Q_OUT = (HAVE < NQ - 1 ? HAVE : NQ - 1) - 1;
-        constexpr int OUT = P_OUT * PL + (Q_OUT > 0 ? Q_OUT : 0) * QL + (HAVE >= NQ ? AT_ONCE : 0);
+        constexpr int HAVE = decltype(slabs_tag)::value;   // slabs, at most ND
+        constexpr int D_OUT = (HAVE < ND - 1 ? HAVE : ND - 1) - 1, F_OUT = (HAVE < NF - 1 ? HAVE : NF - 1) - 1;
+        constexpr int OUT = D_OUT * DL + (F_OUT > 0 ? F_OUT : 0) * FL + (HAVE >= NF ? AT_ONCE : 0);
         wait_loads<OUT>();
     };
-    static_assert(NQ >= 2, "the first part of Q is requested whole");
-    if (S >= NP)
-        begin(std::integral_constant<int, NP>{});
-    else if (NP > 4 && S == 4)
-        begin(std::integral_constant<int, (NP > 4 ? 4 : 1)>{});
-    else if (NP > 3 && S == 3)
-        begin(std::integral_constant<int, (NP > 3 ? 3 : 1)>{});
+    static_assert(NF >= 2, "the follower's first part is requested whole");
+    if (S >= ND)
+        begin(std::integral_constant<int, ND>{});
+    else if (ND > 4 && S == 4)
+        begin(std::integral_constant<int, (ND > 4 ? 4 : 1)>{});
+    else if (ND > 3 && S == 3)
+        begin(std::integral_constant<int, (ND > 3 ? 3 : 1)>{});
     else if (S == 2)
         begin(std::integral_constant<int, 2>{});
     else
@@ -452,31 +471,32 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
 
     Frags f0, f1;
     for_each<0, READS>([&](auto x) __attribute__((always_inline)) { read_one(f0, 0, 0, 0, x); });
-    int pu = 0, qu = 0, pu_old = NP - 1, qu_old = NQ - 1;   // ring places of slab s and of slab s - 1
+    int du = 0, fu = 0, du_old = ND - 1, fu_old = NF - 1;   // ring places of slab s and of slab s - 1
     // LEFT: how many slabs follow; STEADY stands for that and more, and never requests the last slab.
-    constexpr int STEADY = LEAD == 0 ? NP + 1 : NP;
+    constexpr int STEADY = LEAD == 0 ? ND + 1 : ND;
     auto slab_body = [&](int s, auto left_tag) __attribute__((always_inline)) {
         constexpr int LEFT = decltype(left_tag)::value;
         constexpr auto LAST = std::integral_constant<bool, (LEFT < STEADY)>{};
-        constexpr bool OLD_Q = LEFT >= NQ - 1, OLD_P = LEFT >= NP - 1, NEW_Q = LEFT >= NQ;   // what iterations s - 1 and s request
-        const int pu1 = pu + 1 == NP ? 0 : pu + 1, qu1 = qu + 1 == NQ ? 0 : qu + 1;
+        constexpr bool OLD_F = LEFT >= NF - 1, OLD_D = LEFT >= ND - 1, NEW_F = LEFT >= NF;   // what iterations s - 1 and s request
+        const int du1 = du + 1 == ND ? 0 : du + 1, fu1 = fu + 1 == NF ? 0 : fu + 1;
+        const int pu = Q_LEADS ? fu : du, qu = Q_LEADS ? du : fu, pu1 = Q_LEADS ? fu1 : du1, qu1 = Q_LEADS ? du1 : fu1;
         // what goes with instruction POS of the 2 N since a barrier: its share of the loads, in their order
         auto old_loads = [&](auto pos) __attribute__((always_inline)) {
             constexpr int POS = decltype(pos)::value;
             for_each<(POS * NL + 2 * N - 1) / (2 * N), ((POS + 1) * NL + 2 * N - 1) / (2 * N)>([&](auto x) __attribute__((always_inline)) {
                 constexpr int X = decltype(x)::value;
-                if constexpr (X < QL) {
-                    if constexpr (OLD_Q)
-                        load_q(qu_old, s - 1 + NQ, X, LAST);
-                } else if constexpr (OLD_P) {
-                    load_p(pu_old, s - 1 + NP, X - QL, LAST);
+                if constexpr (X < FL) {
+                    if constexpr (OLD_F)
+                        load(FOLLOWER, fu_old, s - 1 + NF, X, LAST);
+                } else if constexpr (OLD_D) {
+                    load(LEADER, du_old, s - 1 + ND, X - FL, LAST);
                 }
             });
         };
-        if (OLD_Q)
-            Q.begin_slab(s - 1 + NQ);
-        if (OLD_P)
-            P.begin_slab(s - 1 + NP);
+        if (OLD_F)
+            begin_slab(FOLLOWER, s - 1 + NF);
+        if (OLD_D)
+            begin_slab(LEADER, s - 1 + ND);
         for_each<0, N>([&](auto n) __attribute__((always_inline)) {   // K step 0
             constexpr int I = decltype(n)::value;
             old_loads(std::integral_constant<int, N / 2 + I>{});
@@ -491,27 +511,27 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
         });
         if constexpr (LEFT > 0) {
             // slab s + 1 has landed, and this wavefront holds its last fragments of slab s
-            constexpr int Q_OUT = (LEFT < NQ - 1 ? LEFT : NQ - 1) - 1, P_OUT = (LEFT < NP - 1 ? LEFT : NP - 1) - 1;
-            wait_loads<Q_OUT * QL + P_OUT * PL>();
+            constexpr int F_OUT = (LEFT < NF - 1 ? LEFT : NF - 1) - 1, D_OUT = (LEFT < ND - 1 ? LEFT : ND - 1) - 1;
+            wait_loads<F_OUT * FL + D_OUT * DL>();
             block_barrier();
-            if (NEW_Q)
-                Q.begin_slab(s + NQ);
+            if (NEW_F)
+                begin_slab(FOLLOWER, s + NF);
         }
         for_each<0, N / 2>([&](auto n) __attribute__((always_inline)) {   // K step 1, second half
             constexpr int I = decltype(n)::value;
-            if constexpr (NEW_Q)
+            if constexpr (NEW_F)
                 for_each<(I * NL + 2 * N - 1) / (2 * N), ((I + 1) * NL + 2 * N - 1) / (2 * N)>(
-                    [&](auto x) __attribute__((always_inline)) { load_q(qu, s + NQ, x, LAST); });
+                    [&](auto x) __attribute__((always_inline)) { load(FOLLOWER, fu, s + NF, x, LAST); });
             if constexpr (LEFT > 0)
                 for_each<(I * READS + N / 2 - 1) / (N / 2), ((I + 1) * READS + N / 2 - 1) / (N / 2)>(
                     [&](auto x) __attribute__((always_inline)) { read_one(f0, pu1, qu1, 0, x); });
             multiply(f1, std::integral_constant<int, N / 2 + I>{});
             __builtin_amdgcn_sched_barrier(0);
         });
-        pu_old = pu;
-        qu_old = qu;
-        pu = pu1;
-        qu = qu1;
+        du_old = du;
+        fu_old = fu;
+        du = du1;
+        fu = fu1;
     };
     // (the first slab on its own: with one loop the compiler gives the accumulators other registers in every slab and moves
     // them back)
@@ -539,7 +559,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     last(std::integral_constant<int, 2>{});
     last(std::integral_constant<int, 1>{});
     last(std::integral_constant<int, 0>{});
-    static_assert(NP <= 5, "every number of slabs left has its body");
+    static_assert(ND <= 5, "every number of slabs left has its body");
     }
 
     // ---- epilogue.  A wavefront passes strips of 16 rows through LDS of its own, as f32, so that a lane finishes 16 bytes
