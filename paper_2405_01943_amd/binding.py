@@ -477,6 +477,7 @@ def down_proj_sparse24(Y: torch.Tensor, values: torch.Tensor, meta: torch.Tensor
 
 # ------------------------------------------------- a mixture of GLU experts --
 _I32 = torch.int32
+_NEEDS_WORKSPACE = 6     # DASS_ERR_WORKSPACE
 
 
 def _on_device(stream, *tensors) -> int:
@@ -518,12 +519,11 @@ def expert_sort(experts: torch.Tensor, n_experts: int, offsets: torch.Tensor, or
     _integers(order, "order", (T * k,))
     _integers(place, "place", (T, k))
     handle = _on_device(stream, experts, offsets, order, place, workspace)
-    if workspace is None:
-        need = int(lib.dass_expert_sort_workspace_bytes(T, k, n_experts))
-        if need > 0:
-            workspace = _scratch(need, experts.device, stream)
-    status = lib.dass_expert_sort(_ptr(experts), experts.element_size(), T, k, n_experts, _ptr(offsets), _ptr(order),
-                                  _ptr(place), _ptr(workspace), _nbytes(workspace), handle)
+    args = _ptr(experts), experts.element_size(), T, k, n_experts, _ptr(offsets), _ptr(order), _ptr(place)
+    status = lib.dass_expert_sort(*args, _ptr(workspace), _nbytes(workspace), handle)
+    if status == _NEEDS_WORKSPACE and workspace is None:    # few pairs need none, so they are not asked first
+        workspace = _scratch(int(lib.dass_expert_sort_workspace_bytes(T, k, n_experts)), experts.device, stream)
+        status = lib.dass_expert_sort(*args, _ptr(workspace), _nbytes(workspace), handle)
     if status:
         _check(status)
 
@@ -649,13 +649,12 @@ def linear(X: torch.Tensor, W: torch.Tensor, out: torch.Tensor, act: str = "none
     ldp, ldo = _like(pre_out, "pre_out", shape, dt), _like(out, "out", shape, dt)
     _bias(bias, "bias", E, d_out, dt)
     handle = _on_device(stream, X, W, out, bias, mul, residual, pre_out, offsets, workspace)
-    if workspace is None:
-        need = int(lib.dass_linear_workspace_bytes(T, d_in, d_out, DTYPE[dt], max(E, 1)))
-        if need > 0:
-            workspace = _scratch(need, X.device, stream)
     task = LinearTask(_ptr(X), T, ldx, _ptr(W), ldw, per_expert, d_in, d_out, _ptr(offsets), max(E, 1), _ptr(bias), _ptr(mul),
                       ldm, _ptr(residual), ldr, _ptr(pre_out), ldp, _ptr(out), ldo, DTYPE[dt], code)
     status = lib.dass_linear(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), handle)
+    if status == _NEEDS_WORKSPACE and workspace is None:    # most calls need none, so they are not asked first
+        workspace = _scratch(int(lib.dass_linear_workspace_bytes(T, d_in, d_out, DTYPE[dt], max(E, 1))), X.device, stream)
+        status = lib.dass_linear(ctypes.byref(task), _ptr(workspace), _nbytes(workspace), handle)
     if status:
         _check(status)
 

@@ -295,10 +295,12 @@ static dass_status launch_sort(const void *ids, int64_t pairs, int E, int32_t *o
     while ((1 << bits) < E)
         ++bits;
     const size_t lds = (size_t)kSortWaves * (E + 1) * 4;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_place_kernel<ID>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * (kMaxExperts + 1) * 4);
-    if (e != hipSuccess)
-        return fail(DASS_ERR_HIP, "sort place kernel: %s", hipGetErrorString(e));
+    if (lds > 48 * 1024) {   // beyond what a launch gets without asking (asking takes 0.9 us of every call)
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_place_kernel<ID>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * (kMaxExperts + 1) * 4);
+        if (e != hipSuccess)
+            return fail(DASS_ERR_HIP, "sort place kernel: %s", hipGetErrorString(e));
+    }
     hipLaunchKernelGGL(sort_place_kernel<ID>, dim3(blocks), dim3(kSortThreads), lds, stream, p, pairs, per_block, E, bits,
                        alone ? nullptr : counts, offsets, order, place);
     return check_launch("sort place kernel");

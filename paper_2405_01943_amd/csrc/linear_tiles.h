@@ -36,6 +36,7 @@
 #include "tile_order.h"
 
 #include <cstdlib>
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -709,6 +710,25 @@ __global__ __launch_bounds__(256) void join_kernel(const Operands<T_> a, const E
 }
 
 // ------------------------------------------------------------------ host side --
+// All of a compute unit's LDS for a kernel: asked for once on every device (0.9 us of a call otherwise).
+template <typename T_, Product PRODUCT, int RB, int CB>
+static hipError_t reserve_lds()
+{
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess)
+        return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit)
+        return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_tile_kernel<T_, PRODUCT, RB, CB>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e == hipSuccess)
+        done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 template <typename T_, Product PRODUCT, int RB, int CB>
 static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, const Split &split, hipStream_t stream)
 {
@@ -725,8 +745,7 @@ static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epi
     const unsigned experts = PRODUCT == kWeightGrad ? a.seg.n : 1;
     if (order.blocks == 0 || (int64_t)order.blocks * 256 > 0xffffffffLL / experts / split.n)
         return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_tile_kernel<T_, PRODUCT, RB, CB>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    const hipError_t e = reserve_lds<T_, PRODUCT, RB, CB>();
     if (e != hipSuccess)
         return fail(DASS_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", fn, kLds, hipGetErrorString(e));
     hipLaunchKernelGGL((product_tile_kernel<T_, PRODUCT, RB, CB>), dim3(order.blocks, experts, split.n), dim3(256), kLds, stream, a, ep,
