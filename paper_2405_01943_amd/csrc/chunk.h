@@ -1,4 +1,4 @@
-// One 16-byte chunk of a row (8 bf16 or 4 f32) as f32 values and back, and the f32 value of one element.
+// One 16-byte chunk of a row (8 bf16 or 4 f32) as f32 values and back.
 #pragma once
 
 #include <hip/hip_runtime.h>

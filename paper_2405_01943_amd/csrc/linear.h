@@ -201,7 +201,7 @@ struct Split {
 // Which kernel a product takes (plan_product in linear.hip).
 struct Plan {
     enum Kind { kTiles, kFew } kind;
-    int tile;     // kTiles: 0: 256 x 256, 1: 128 x 256, 2: 128 x 128 (f32: always 2)
+    int tile;     // kTiles: 0: 256 x 256, 1: 128 x 256, 2: 128 x 128 (f32: always 2), 3: 128 x 128, two a compute unit
     int splits;   // kTiles: shares of k
     int blocks;   // kFew: 16-row (and in f32 16-column) blocks of a workgroup
 };

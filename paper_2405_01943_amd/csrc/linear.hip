@@ -211,52 +211,62 @@ struct Checker {
 };
 
 // The kernel, the tile and the split of k that are expected to be fastest for the products of `groups` experts: cols columns,
-// `depth` of k each, and `rows` rows each (dW) or all together.  The estimates, in us, are lines through times of 90 bf16 and 45
-// f32 products of 1 to 16384 rows and every tile with 1 to 16 shares; over these the choice is 1 % slower than the best in
-// the mean, 31 % at the worst (dX of 16 rows an expert).
+// `depth` of k each, and `rows` rows each (dW) or all together.  The estimates, in us, are fitted to times of 149 bf16 and 45
+// f32 products of 1 to 16384 rows and every tile with 1 to 16 shares; over the bf16 ones the choice is 1 % slower than the best
+// in the mean, 27 % at the worst (dX of 8 rows for each of 64 experts of 2048 x 1408).
 //
-//   tiles   rounds of 256 workgroups x (start + slabs x slab), and with a split 8 bytes for each share's sum (written and
-//           read) and the second launch.  A tile's slab takes as long as its bytes from L2, whichever shape; large
-//           tiles read least in all, small ones and shares fill the chip.  1024 rows of 4096 x 4096, 256 x 256 / 128 x
-//           256 / 128 x 128: 93 / 56 / 39 us, 52 / 46 / 55 with 4, 2 and 2 shares; 16384 rows of 4096 x 11008: 1197 us with
-//           256 x 256; dX of 6000 rows of 4096 x 11008 473 / 503 / -; 64 rows of 11008 x 4096 (128 x 128) 88 us, 27 with 8 shares; dW of 16384 rows of 512 x 512 145, 28
-//           with 8; one share where the tiles fill the chip: 2048 rows of 4096 x 4096 59 us, 86 with 2.
+//   tiles   rounds of `slots` workgroups x (start + slabs x slab), or what memory takes for the weights and the output, and with a
+//           split 8 bytes for each share's sum (written and read) and the second launch.  A tile's slab takes as long as its
+//           bytes from L2, whichever shape; large tiles read least in all, small ones and shares fill the chip.  1024 rows of
+//           4096 x 4096, 256 x 256 / 128 x 256 / 128 x 128: 93 / 56 / 39 us, 52 / 46 / 55 with 4, 2 and 2 shares; 16384
+//           rows of 4096 x 11008: 1197 us with 256 x 256; dX of 6000 rows of 4096 x 11008 473 / 503 / -; 64 rows of 11008 x
+//           4096 (128 x 128) 88 us, 27 with 8 shares; dW of 16384 rows of 512 x 512 145, 28 with 8; one share where the
+//           tiles fill the chip: 2048 rows of 4096 x 4096 59 us, 86 with 2.
+//   short   (bf16) two 128 x 128 workgroups a compute unit with shorter rings: one's stores run beside the other's products, so
+//           it leads where k is short, 8192 rows of 64 x 4096 26 us (the best other tile 36), 512 x 4096 49 (52), 1024 x
+//           4096 74 (72); and alone on a compute unit its slabs are slower than the others': no shares.
 //   few     (f32) a fixed part that grows with k, or the workgroups and their multiplications.  512 rows of 256 x 688: blocks
 //           of 16 / of 32 / tiles 13.2 / 6.7 / 16.6 us, 16 of 1024 x 1024 5.7 / 8.9 / 11.5, 1024 of 512 x 512 17 / 10 / 19,
 //           4096 of 1024 x 1024 225 / 119 / 71.
-//           (bf16, forward only) the weights' bytes, or one workgroup's.  Up to 8 rows: one row of 4096 x 11008 17.7 us (tiles
-//           with 4 shares 24), 8 of it 22.2 (24), 16 of it 27 (24); 16384 x 256 19.6 with 16 workgroups (tiles with 16
-//           shares 13.4).  One row an expert: 8 rows over 5 experts of 4096 x 14336 98 (130), but 16 over 8 170 (163).
+//           (bf16, forward only) the weights' bytes, or one workgroup's.  Up to 8 rows: one row of 2048 x 32000 30.0 us (tiles
+//           36.5), 8 of it 34.5 (37.7); but one row of 16384 x 1024 20.6 (tiles with 16 shares 15.6).  16 rows over 8 experts
+//           of 4096 x 14336 171 (186), 64 over 8 204 (182).
 static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, int64_t cols, int64_t depth)
 {
     const bool bf16 = dt == DASS_BF16;
     const auto pieces = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
     const int64_t share = product == kWeightGrad ? rows : pieces(rows, groups);   // of an expert, were they even
+    const int64_t used = std::min(groups, rows);
     // the row tiles of experts of uneven size: half a tile more each
     const auto row_tiles = [&](int64_t of) {
         if (product == kWeightGrad || groups == 1)
             return groups * pieces(rows, of);
-        return std::max(groups, rows / of + groups / 2);
+        return std::max(used, rows / of + used / 2);
     };
 
     static const int kShares[] = {1, 2, 3, 4, 6, 8, 12, 16};
     static const struct {
-        int rows, cols;
+        int rows, cols, slots;   // slots: workgroups that the card holds
         double start, slab;
-    } kTiles[] = {{256, 256, 5.4, 1.0}, {128, 256, 3.3, 0.67}, {128, 128, 1.9, 0.435}}, kTileF32 = {128, 128, 3.4, 2.49};
-    const double join = bf16 ? 4.4 : 2.4, byte = bf16 ? 1 / 6.9e6 : 1 / 4.5e6;   // us, us a byte
+    } kTiles[] = {{256, 256, 256, 8.8, 1.34}, {128, 256, 256, 5.4, 0.87}, {128, 128, 256, 4.06, 0.517}, {128, 128, 512, 3.47, 0.985}},
+      kTileF32 = {128, 128, 256, 3.4, 2.49};
+    const double join = bf16 ? 3.64 : 2.4, byte = bf16 ? 1 / 6.13e6 : 1 / 4.5e6;   // us, us a byte
     const int64_t slabs = pieces(depth, bf16 ? 64 : 32), outputs = (product == kWeightGrad ? groups : 1) * rows * cols;
-    const double weights = product == kWeightGrad ? 0 : (bf16 ? 2.0 : 4.0) * groups * cols * depth / 4.6e6;   // out of memory
+    const double weights = product == kWeightGrad ? 0 : (bf16 ? 6 : 0) + (bf16 ? 2.0 / 5.2e6 : 4.0 / 4.6e6) * used * cols * depth;
+    const double written = bf16 ? 2.0 / 3.38e6 * outputs : 0;
     Plan best = {Plan::kTiles, bf16 ? 0 : 2, 1, 0};
     double best_time = 1e300;
-    for (int k = bf16 ? 0 : 2; k < 3; ++k) {
+    for (int k = bf16 ? 0 : 2; k < (bf16 ? 4 : 3); ++k) {
         const auto &t = bf16 ? kTiles[k] : kTileF32;
         const int64_t tiles = row_tiles(t.rows) * pieces(cols, t.cols);
         for (const int z : kShares) {
-            if (z > 1 && (slabs < 2 * z || (double)z * outputs * 4 > 256e6))
+            if (z > 1 && (k == 3 || slabs < 2 * z || (double)z * outputs * 4 > 256e6))
                 break;
-            const double busy = pieces(tiles * z, 256) * (t.start + pieces(slabs, z) * t.slab);
-            const double time = std::max(busy, weights) + (z > 1 ? join + z * 8.0 * outputs * byte : 0);
+            // alone on its compute unit a workgroup of the short tile is not held up by a second
+            const double one = k == 3 && tiles <= 256 ? 4.47 + slabs * 0.689 : t.start + pieces(slabs, z) * t.slab;
+            const double busy = pieces(tiles * z, t.slots) * one, memory = weights + (z == 1 ? written : 0);
+            const double time = std::max(busy, memory) + (bf16 ? 0.093 * std::min(busy, memory) : 0) +
+                                (z > 1 ? join + z * 8.0 * outputs * byte : 0);
             if (time < best_time) {
                 best_time = time;
                 best = {Plan::kTiles, k, z, 0};
@@ -264,8 +274,8 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
         }
     }
     if (bf16 && product == kForward && share <= 8) {
-        const double bytes = 2.0 * groups * cols * depth * (1 + 0.035 * (share - 1));
-        if ((share == 1 && groups > 1) || std::max(2 + 0.0011 * depth, bytes / 4.9e6) < best_time)
+        const double bytes = 2.0 * used * cols * depth * (1 + 0.025 * (share - 1));
+        if ((share == 1 && groups > 1) || std::max(2 + 0.0011 * depth, 2 + bytes / 5.1e6) < best_time)
             return {Plan::kFew, 0, 1, 1};
     }
     for (int blocks = 1; !bf16 && blocks <= 2; ++blocks) {

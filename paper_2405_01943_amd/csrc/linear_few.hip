@@ -5,8 +5,7 @@
 // come straight from global memory (each is used by one wavefront alone, so LDS would only add a trip): lane l of a
 // fragment holds 16 bytes of row l % 16, k = 4 (8 for bf16) (l / 16) .. of 16 (32), two fragments of a row side by side are
 // a 128-byte line, and the wavefronts take these lines in turn.  For one token the weights are all there is to read: the
-// kernel's time is theirs.  Stored k by k (f32 only), the four k of a lane are four 4-byte loads.  The matrix instructions and their
-// operands' pairing of k are those of linear_f32.hip and linear_bf16.hip.
+// kernel's time is theirs.  Stored k by k (f32 only), the four k of a lane are four 4-byte loads.
 #include "linear.h"
 
 namespace dass {

@@ -17,16 +17,17 @@
 //             bytes of line k lie in place piece ^ (k / 4 mod 4), so that the four lines of a read meet all banks once.
 // So no operand is transposed in memory: the three products (linear.h) differ in their operands' forms alone.
 //
-// LDS is two rings, ND parts of the operand that leads and NF of the one that follows, as many as 160 KB hold.  The places of slab s are free after the one
-// barrier of the slab, which stands where every wavefront has read its last fragments of it, in the middle of its second
-// K step; the loads of the follower's slab s + NF and the leader's s + ND are spread over the matrix instructions from there to the
-// next barrier.  The wait before a barrier counts the loads that may still be on their way, so their order is
-// pinned; only slabs that exist are requested, and the last slabs have bodies of their own with fewer to wait for.
+// LDS is two rings, ND parts of the operand that leads and NF of the one that follows, as many as 160 KB hold (in the short tiles
+// 64 KB).  The places of slab s are free after the one barrier of the slab, which stands where every wavefront has read its
+// last fragments of it, in the middle of its second K step; the loads of the follower's slab s + NF and the leader's s + ND
+// are spread over the matrix instructions from there to the next barrier.  The wait before a barrier counts the loads that
+// may still be on their way, so their order is pinned; only slabs that exist are requested, and the last slabs have bodies
+// of their own with fewer to wait for.
 //
 // Reads outside a matrix: each operand is a raw buffer that starts at the tile's first row and ends with its last
 // valid element; what lies beyond reads as 0.  Lane offsets are 32-bit registers, the scalar offset is at most a row
-// (by rows) or none (k by k, whose buffer moves with the slab), so the length less the scalar offset is never negative.  By rows, chunks of
-// the last slab that lie beyond k are given an offset outside the buffer.
+// (by rows) or none (k by k, whose buffer moves with the slab), so the length less the scalar offset is never negative.  By
+// rows, chunks of the last slab that lie beyond k are given an offset outside the buffer.
 //
 // Grids of few tiles split k over blockIdx.z: each share writes its sums as f32 to a place of its own in the workspace, and a second
 // launch adds them up in order and finishes the outputs (join_kernel).
@@ -62,7 +63,12 @@ __device__ __forceinline__ void for_each(F &&f)
                     std::make_integer_sequence<int, TO - FROM>{});
 }
 
-constexpr int kLds = 160 * 1024, kSlabBytes = 128;
+constexpr int kSlabBytes = 128;
+template <bool SHORT>
+constexpr int lds_bytes()
+{
+    return (SHORT ? 64 : 160) * 1024;
+}
 constexpr int kOutside = 0x7fffffff;
 
 // A raw buffer: 48 bits of address, no stride, its length in bytes.
@@ -258,10 +264,21 @@ __device__ __forceinline__ f32x4 multiply_add(const u32x4 &q, const u32x4 &p, f3
     return acc;
 }
 
+__device__ __forceinline__ void store(void *p, const u32x4 &v, bool streamed)
+{
+    if (streamed) {
+        asm volatile("");   // on both sides, or the compiler makes one plain store of the two
+        __builtin_nontemporal_store(v, static_cast<u32x4 *>(p));
+        asm volatile("");
+    } else {
+        *static_cast<u32x4 *>(p) = v;
+    }
+}
+
 // The epilogue of one 16-byte chunk of a row (8 bf16, 4 f32), with the chunks of mul and residual at hand; `col` is inside.
 template <typename T_, int N = Chunk<T_>::N>
-__device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int64_t col, const float (&bias)[N], const u32x4 &mul,
-                                       const u32x4 &residual, float (&v)[N])
+__device__ __forceinline__ void finish(const Epilogue<T_> &ep, bool streamed, int64_t row, int64_t col, const float (&bias)[N],
+                                       const u32x4 &mul, const u32x4 &residual, float (&v)[N])
 {
     typedef Chunk<T_> C;
     constexpr bool FAST = sizeof(T_) == 2;
@@ -272,7 +289,7 @@ __device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int6
             v[i] += bias[i];
     }
     if (ep.pre)
-        __builtin_nontemporal_store(C::narrow(v), reinterpret_cast<u32x4 *>(ep.pre + row * ep.ldp + col));
+        store(ep.pre + row * ep.ldp + col, C::narrow(v), streamed);
     act_values<FAST>(v, ep.act);
     if (ep.mul) {
         C::widen(mul, w);
@@ -286,7 +303,7 @@ __device__ __forceinline__ void finish(const Epilogue<T_> &ep, int64_t row, int6
         for (int i = 0; i < N; ++i)
             v[i] += w[i];
     }
-    __builtin_nontemporal_store(C::narrow(v), reinterpret_cast<u32x4 *>(ep.out + row * ep.ldo + col));
+    store(ep.out + row * ep.ldo + col, C::narrow(v), streamed);
 }
 
 // Every XCD one contiguous run of the tiles, as tile_order.h has them, for a number of row tiles that only the device knows.
@@ -301,7 +318,9 @@ __device__ __forceinline__ TileOrder order_runs(uint32_t tiles_r, uint32_t tiles
     return o;
 }
 
-template <typename T_, Product PRODUCT, int RB, int CB>
+// SHORT: rings of two parts each, 64 KB in all, so that two workgroups share a compute unit and one's loads and stores go on
+// beside the other's products: for k of few slabs.
+template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT>
 __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a, const Epilogue<T_> ep0, const TileOrder order, const Split split)
 {
     constexpr bool BY_HAND = sizeof(T_) == 2 && PRODUCT != kForward;   // transposing reads
@@ -313,12 +332,13 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     // 11008 486 -> 475 us, over 8 experts 541 -> 533; in the forward product they do not (8192 rows of 4096 x 14336 690, with
     // them 699; over 8 experts 880 and 867).
     constexpr bool Q_LEADS = RB == 8 && PRODUCT == kInputGrad;
-    constexpr int ND = RB == 8 ? 3 : CB == 8 ? 4 : 5, NF = RB == 8 ? 2 : CB == 8 ? 3 : 5, LEAD = ND - NF;
+    constexpr int ND = SHORT ? 2 : RB == 8 ? 3 : CB == 8 ? 4 : 5, NF = SHORT || RB == 8 ? 2 : CB == 8 ? 3 : 5, LEAD = ND - NF;
+    constexpr int LDS = lds_bytes<SHORT>();
     constexpr int NP = Q_LEADS ? NF : ND, NQ = Q_LEADS ? ND : NF;
-    static_assert(NP * PartP::UNIT + NQ * PartQ::UNIT <= kLds && (LEAD == 0 || LEAD == 1), "the rings fit");
+    static_assert(NP * PartP::UNIT + NQ * PartQ::UNIT <= LDS && (LEAD == 0 || LEAD == 1), "the rings fit");
     constexpr int DL = Q_LEADS ? PartQ::LOADS : PartP::LOADS, FL = Q_LEADS ? PartP::LOADS : PartQ::LOADS, NL = DL + FL;
     constexpr int N = RB * CB;   // matrix instructions of a K step
-    extern __shared__ __attribute__((aligned(1024))) char lds[];   // kLds bytes
+    extern __shared__ __attribute__((aligned(1024))) char lds[];   // LDS bytes
 
     uint32_t tile_r, tile_c;   // tile_order.h
     int expert = 0;
@@ -569,10 +589,10 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     // fetched anew (4096 rows of 512 x 4096 37 us).  mul and residual are requested a strip ahead.
     constexpr int N_CHUNK = Chunk<T_>::N;
     constexpr int SROW = 16 * CB * 4 + 16, LANES = 16 * CB / N_CHUNK, ROWS = 64 / LANES;   // lanes of a row; rows of a read
-    constexpr int READS_16 = 16 / ROWS, HELD = RB < 4 ? RB : 4;
-    static_assert(ROWS * LANES == 64 && HELD * 16 * SROW <= kLds / 4 && RB % HELD == 0, "strips");
+    constexpr int READS_16 = 16 / ROWS, HELD = SHORT ? 2 : 4;
+    static_assert(ROWS * LANES == 64 && HELD * 16 * SROW <= LDS / 4 && RB % HELD == 0, "strips");
     Epilogue<T_> ep = ep0;
-    char *const strips = lds + wave * (kLds / 4);
+    char *const strips = lds + wave * (LDS / 4);
     const int fr = lane & 15, g = lane >> 4;
     int64_t row = r0 + wr * 16 * RB + lane / LANES;
     const int64_t col = c0 + wc * 16 * CB + lane % LANES * N_CHUNK;
@@ -582,6 +602,11 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
         share += (int64_t)expert * a.out_rows * ep.cols;
     }
     const bool whole = split.n == 1;
+    // Stores that bypass the caches leave L2 to the operands (dW of 6000 rows over 8 experts of 4096 x 11008 536 us, 559 without;
+    // 8192 rows of 128 x 4096 28.3, 31.3), but write a row's ends in pieces where it does not begin and end on lines, and those
+    // cost more than a line that L2 puts together (dW of 7 rows over 18 experts of 3496 x 7456 416 us, 218 through L2).
+    const uint64_t begins = reinterpret_cast<uintptr_t>(ep.out) | reinterpret_cast<uintptr_t>(ep.pre) | (ep.ldo | ep.ldp) * sizeof(T_);
+    const bool streamed = begins % 128 == 0;
     float bias[N_CHUNK];
 #pragma unroll
     for (int i = 0; i < N_CHUNK; ++i)
@@ -640,9 +665,9 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
                         for (int i = 0; i < N_CHUNK / 4; ++i)
                             *reinterpret_cast<f32x4 *>(split.partial + share + r * ep.cols + col + 4 * i) = part[i];
                     } else if constexpr (PRODUCT == kForward) {
-                        finish(ep, r, col, bias, mul_now[t], residual_now[t], v);
+                        finish(ep, streamed, r, col, bias, mul_now[t], residual_now[t], v);
                     } else {
-                        __builtin_nontemporal_store(Chunk<T_>::narrow(v), reinterpret_cast<u32x4 *>(ep.out + r * ep.ldo + col));
+                        store(ep.out + r * ep.ldo + col, Chunk<T_>::narrow(v), streamed);
                     }
                 }
             }
@@ -704,14 +729,14 @@ __global__ __launch_bounds__(256) void join_kernel(const Operands<T_> a, const E
     for (int i = 0; i < N; ++i)
         v[i] = sum[i / 4][i % 4];
     if constexpr (PRODUCT == kForward)
-        finish(ep, row, col, bias, mul, residual, v);
+        finish(ep, false, row, col, bias, mul, residual, v);
     else
         *reinterpret_cast<u32x4 *>(out + out_row * ep.ldo + col) = Chunk<T_>::narrow(v);
 }
 
 // ------------------------------------------------------------------ host side --
-// All of a compute unit's LDS for a kernel: asked for once on every device (0.9 us of a call otherwise).
-template <typename T_, Product PRODUCT, int RB, int CB>
+// More LDS than a launch gets without asking: asked for once a kernel and device (0.9 us of a call otherwise).
+template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT>
 static hipError_t reserve_lds()
 {
     static std::atomic<uint64_t> done{0};
@@ -722,14 +747,14 @@ static hipError_t reserve_lds()
     const uint64_t bit = device < 64 ? 1ull << device : 0;
     if (done.load(std::memory_order_relaxed) & bit)
         return hipSuccess;
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_tile_kernel<T_, PRODUCT, RB, CB>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_tile_kernel<T_, PRODUCT, RB, CB, SHORT>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<SHORT>());
     if (e == hipSuccess)
         done.fetch_or(bit, std::memory_order_relaxed);
     return e;
 }
 
-template <typename T_, Product PRODUCT, int RB, int CB>
+template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT = false>
 static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, const Split &split, hipStream_t stream)
 {
     constexpr int BR = 32 * RB, BC = 32 * CB;
@@ -745,11 +770,11 @@ static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epi
     const unsigned experts = PRODUCT == kWeightGrad ? a.seg.n : 1;
     if (order.blocks == 0 || (int64_t)order.blocks * 256 > 0xffffffffLL / experts / split.n)
         return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
-    const hipError_t e = reserve_lds<T_, PRODUCT, RB, CB>();
+    const hipError_t e = reserve_lds<T_, PRODUCT, RB, CB, SHORT>();
     if (e != hipSuccess)
-        return fail(DASS_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", fn, kLds, hipGetErrorString(e));
-    hipLaunchKernelGGL((product_tile_kernel<T_, PRODUCT, RB, CB>), dim3(order.blocks, experts, split.n), dim3(256), kLds, stream, a, ep,
-                       order, split);
+        return fail(DASS_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", fn, lds_bytes<SHORT>(), hipGetErrorString(e));
+    hipLaunchKernelGGL((product_tile_kernel<T_, PRODUCT, RB, CB, SHORT>), dim3(order.blocks, experts, split.n), dim3(256),
+                       lds_bytes<SHORT>(), stream, a, ep, order, split);
     dass_status s = check_launch("product kernel");
     if (s != DASS_OK || split.n == 1)
         return s;
@@ -771,6 +796,8 @@ static dass_status launch_plan(const char *fn, const Plan &plan, const Operands<
             return launch_tiles<T_, PRODUCT, 8, 8>(fn, a, ep, split, stream);
         if (plan.tile == 1)
             return launch_tiles<T_, PRODUCT, 4, 8>(fn, a, ep, split, stream);
+        if (plan.tile == 3)
+            return launch_tiles<T_, PRODUCT, 4, 4, true>(fn, a, ep, split, stream);
     }
     return launch_tiles<T_, PRODUCT, 4, 4>(fn, a, ep, split, stream);
 }

@@ -109,11 +109,15 @@ def test_linear_sizes(gpu_device, T, d_in, d_out, dtype):
 
 
 # Larger grids: together, and with SIZES, they take every kernel: in bf16 the tiles of 256 x 256, 128 x 256 and 128 x 128, k whole
-# and split (2 to 12 shares), in f32 the tiles and both sizes of blocks, for the product and both gradients
+# and split (2 to 16 shares), and the short 128 x 128, in f32 the tiles, whole and split, and both sizes of blocks, for the
+# product and both gradients
 LARGE = [("bf16", 4224, 136, 4104, 0), ("bf16", 4100, 2056, 2056, 0), ("bf16", 2050, 264, 2056, 0), ("bf16", 5000, 264, 8200, 0),
          ("bf16", 8200, 520, 1032, 0), ("bf16", 4096, 1032, 4104, 0), ("bf16", 130, 4104, 1032, 0), ("bf16", 9000, 264, 4104, 5),
          ("bf16", 9000, 4104, 264, 5), ("bf16", 12000, 136, 264, 3), ("bf16", 700, 2056, 264, 5), ("f32", 4100, 264, 1032, 0),
-         ("f32", 4100, 1032, 264, 0), ("f32", 9000, 132, 132, 0), ("f32", 9000, 132, 260, 3)]
+         ("f32", 4100, 1032, 264, 0), ("f32", 9000, 132, 132, 0), ("f32", 9000, 132, 260, 3),
+         ("bf16", 2050, 4104, 2056, 0), ("bf16", 4100, 4104, 136, 0), ("bf16", 1000, 72, 4104, 3), ("bf16", 520, 4104, 4104, 0),
+         ("f32", 4096, 264, 1000, 0), ("f32", 4096, 1000, 264, 0), ("f32", 260, 1000, 4096, 0), ("f32", 1000, 6152, 1000, 0),
+         ("f32", 1000, 1000, 6152, 0), ("f32", 6152, 1000, 1000, 0)]
 
 
 @pytest.mark.parametrize("dtype,T,d_in,d_out,E", LARGE)
