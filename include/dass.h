@@ -379,6 +379,7 @@ dass_status dass_down_proj_sparse24(const void *Y, int64_t T, int64_t ldy, const
  * X, out of the gather etc. are rows of d elements of dtype dt; d is a multiple
  * of 8 (bf16) or 4 (f32) up to 2^24.  Entries of place outside 0 .. T k - 1 count as
  * pairs that go nowhere.  place must not hold a row twice where rows are written.
+ * Outputs must not overlap inputs, but for the residual (with its stride).
  */
 size_t dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t n_experts);
 

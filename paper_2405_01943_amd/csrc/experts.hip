@@ -341,6 +341,12 @@ static dass_status check_row_length(const char *fn, int64_t d, dass_dtype dt)
     return DASS_OK;
 }
 
+// An output that begins where an input does.
+static dass_status check_apart(const char *fn, const char *name, const void *out, const void *in)
+{
+    return out != in ? DASS_OK : fail(DASS_ERR_ARG, "%s: %s must not overlap an input", fn, name);
+}
+
 // Workgroups of 256 threads for a number of 16-byte chunks; 0: more than one launch holds.
 static unsigned chunk_blocks(int64_t chunks)
 {
@@ -411,6 +417,9 @@ extern "C" dass_status dass_expert_gather(const void *X, int64_t T, int64_t ldx,
     const unsigned blocks = chunk_blocks(T * chunks);
     if (blocks == 0)
         return fail(DASS_ERR_SHAPE, "%s: too many rows for one launch; split the tokens", fn);
+    s = check_apart(fn, "out", out, X);
+    if (s != DASS_OK)
+        return s;
     hipLaunchKernelGGL(gather_kernel, dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream),
                        static_cast<const char *>(X), ldx * e, (uint32_t)chunks, T * chunks, place, (int)k, T * k,
                        static_cast<char *>(out), ldo * e);
@@ -442,6 +451,11 @@ extern "C" dass_status dass_expert_combine(const void *Y, int64_t ldy, const int
     const unsigned blocks = chunk_blocks(T * chunks);
     if (blocks == 0)
         return fail(DASS_ERR_SHAPE, "%s: too many rows for one launch; split the tokens", fn);
+    s = check_apart(fn, "out", out, Y);
+    if (s == DASS_OK && ldr != ldo)
+        s = check_apart(fn, "out with another stride", out, residual);
+    if (s != DASS_OK)
+        return s;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (dt == DASS_BF16)
         hipLaunchKernelGGL(combine_kernel<uint16_t>, dim3(blocks), dim3(256), 0, stream, static_cast<const uint16_t *>(Y), ldy,
@@ -479,6 +493,13 @@ extern "C" dass_status dass_expert_combine_backward(const void *dout, int64_t ld
     const int64_t blocks = (T + 3) / 4;
     if (blocks > 0xffffffffLL / 256)
         return fail(DASS_ERR_SHAPE, "%s: too many rows for one launch; split the tokens", fn);
+    s = check_apart(fn, "dY", dY, dout);
+    if (s == DASS_OK)
+        s = check_apart(fn, "dY", dY, Y);
+    if (s == DASS_OK)
+        s = check_apart(fn, "dweights", dweights, weights);
+    if (s != DASS_OK)
+        return s;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint32_t chunks = (uint32_t)(d / vec_elems(dt));
     if (dt == DASS_BF16)

@@ -58,6 +58,15 @@ def test_row_rejections(lib):
     assert grad(w=None) == grad(dw=None) == grad(Y=None) == "NULL" and grad(dw=0x10002) == "ALIGN" and grad(ldy=56) == "SHAPE"
 
 
+def test_rows_over_their_inputs(lib):
+    """An output that begins where an input does would be read after it is written."""
+    assert _name(lib, lib.dass_expert_gather(A, 8, 64, 64, 1, B, 2, A, 64, None)) == "ARG"
+    assert _name(lib, lib.dass_expert_combine(A, 64, B, 8, 2, C, None, 0, 64, 1, A, 64, None)) == "ARG"
+    assert _name(lib, lib.dass_expert_combine(A, 64, B, 8, 2, C, D, 72, 64, 1, D, 64, None)) == "ARG"     # the residual's own stride alone
+    for dout, Y, dY, w, dw in ((A, B, A, C, D), (A, B, B, C, D), (A, B, 0x800000, C, C)):
+        assert _name(lib, lib.dass_expert_combine_backward(dout, 64, Y, 64, D, 8, 2, w, 64, 1, dY, 64, dw, None)) == "ARG"
+
+
 def _linear(lib, **change):
     t = dict(X=A, T=8, ldx=64, W=A, ldw=64, expert_stride=0, d_in=64, d_out=64, offsets=None, n_experts=1, bias=None, mul=None, ldm=0,
              residual=None, ldr=0, pre_out=None, ldp=0, out=B, ldo=64, dt=1, act=4)
