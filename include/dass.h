@@ -421,8 +421,9 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  *   workspace  dass_linear_workspace_bytes() bytes, 16-byte aligned (0 and NULL
  *            where the outputs are many; else partial sums over shares of d_in)
  * All of dtype dt (bf16 or f32); sums and epilogue are f32, rounded once (pre
- * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32) up to 2^24,
- * T is below 2^31, row strides are at most 2^36.
+ * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32) up to 2^20, T is
+ * at most 2^30.  Rows of X and W, and of dout below, lie less than 8 MiB apart, others at most
+ * 2^36 elements.
  *
  * dass_linear_backward gives, with g = dout * mul * act'(pre),
  *

@@ -92,9 +92,11 @@ struct TileList {
     {
         int tiles;
         scan = scan_64(s, 0, bm, tiles);
-        total = __builtin_amdgcn_readlane(scan, 63);
+        int64_t sum = __builtin_amdgcn_readlane(scan, 63);
         for (int e0 = 64; e0 < s.n; e0 += 64)
-            total += __builtin_amdgcn_readlane(scan_64(s, e0, bm, tiles), 63);
+            sum += __builtin_amdgcn_readlane(scan_64(s, e0, bm, tiles), 63);
+        const int64_t most = s.rows / bm + s.n;   // (more where offsets fall)
+        total = (int)(sum < most ? sum : most);
     }
     // `tile` below total
     __device__ __forceinline__ Span rows(const Segments &s, int bm, int tile, int &expert) const

@@ -14,7 +14,8 @@
 namespace dass {
 
 constexpr int kMaxLinearExperts = 1024;
-constexpr int64_t kMaxWidth = 1 << 24, kMaxStride = 1LL << 36;   // every product of sizes stays within 64 bits
+constexpr int64_t kMaxRows = 1 << 30, kMaxWidth = 1 << 20, kMaxStride = 1LL << 36;   // products of sizes stay within 64 bits
+constexpr int64_t kMaxReadRow = 1 << 23;   // bytes between rows that a tile addresses: 256 of them with 32-bit offsets
 
 // ------------------------------------------------------ element-wise gradient and sums --
 // A wavefront owns 64 chunks of 16 bytes of columns and every fourth row of a tile of rows of one expert.  One pass:
@@ -149,21 +150,24 @@ static size_t partial_bytes(int64_t rows, int64_t d_out, int64_t n_experts, int 
     return round_up((size_t)(rows / sum_tile_rows(rows, d_out, dt) + 1 + n_experts) * (size_t)d_out * 4, 256);
 }
 
+// The longest row stride of an operand of the products, in elements: 256 of them stay below 2^31 bytes.
+static int64_t longest_read(int dt) { return kMaxReadRow / (dt == DASS_BF16 ? 2 : 4) - vec_elems(dt); }
+
 struct Checker {
     const char *fn;
     int vec;
     dass_status status = DASS_OK;
 
-    // a matrix of `rows` rows of `width` elements; absent optional ones are fine
-    void matrix(const char *name, const void *p, int64_t ld, int64_t width, bool required)
+    // a matrix of rows of `width` elements; absent optional ones are fine
+    void matrix(const char *name, const void *p, int64_t ld, int64_t width, bool required, int64_t longest = kMaxStride)
     {
         if (status != DASS_OK || (!p && !required))
             return;
         if (!p)
             status = fail(DASS_ERR_NULL, "%s: %s must not be NULL", fn, name);
-        else if (ld < width || ld > kMaxStride)
-            status = fail(DASS_ERR_SHAPE, "%s: row stride %lld of %s is shorter than its rows of %lld or beyond 2^36", fn, (long long)ld,
-                          name, (long long)width);
+        else if (ld < width || ld > longest)
+            status = fail(DASS_ERR_SHAPE, "%s: row stride %lld of %s is shorter than its rows of %lld or beyond %lld", fn, (long long)ld,
+                          name, (long long)width, (long long)longest);
         else if (!aligned16(p) || ld % vec != 0)
             status = fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
     }
@@ -188,8 +192,8 @@ struct Checker {
         else if (T <= 0 || d_in <= 0 || d_out <= 0)
             status = fail(DASS_ERR_SHAPE, "%s: T=%lld d_in=%lld d_out=%lld must be positive", fn, (long long)T, (long long)d_in,
                           (long long)d_out);
-        else if (T > 0x7fffffffLL || d_in > kMaxWidth || d_out > kMaxWidth)
-            status = fail(DASS_ERR_SHAPE, "%s: T=%lld must be below 2^31, d_in=%lld and d_out=%lld at most 2^24", fn, (long long)T,
+        else if (T > kMaxRows || d_in > kMaxWidth || d_out > kMaxWidth)
+            status = fail(DASS_ERR_SHAPE, "%s: T=%lld must be at most 2^30, d_in=%lld and d_out=%lld at most 2^20", fn, (long long)T,
                           (long long)d_in, (long long)d_out);
         else if (d_in % vec_elems(dt) != 0 || d_out % vec_elems(dt) != 0)
             status = fail(DASS_ERR_SHAPE, "%s: d_in=%lld and d_out=%lld must be multiples of %d", fn, (long long)d_in,
@@ -273,13 +277,19 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
             }
         }
     }
-    if (bf16 && product == kForward && share <= 8) {
+    const auto one_launch = [&](int of, int threads) {   // of workgroups of `of` x `of` outputs
+        const int64_t most = product == kWeightGrad ? groups * pieces(rows, of) : rows / of + groups;
+        return (double)most * pieces(cols, of) * threads < 0xffffffffu;
+    };
+    if (bf16 && product == kForward && share <= 8 && one_launch(16, 1024)) {
         const double bytes = 2.0 * used * cols * depth * (1 + 0.025 * (share - 1));
         if ((share == 1 && groups > 1) || std::max(2 + 0.0011 * depth, 2 + bytes / 5.1e6) < best_time)
             return {Plan::kFew, 0, 1, 1};
     }
     for (int blocks = 1; !bf16 && blocks <= 2; ++blocks) {
         const double workgroups = (double)row_tiles(16 * blocks) * pieces(cols, 16 * blocks);
+        if (!one_launch(16 * blocks, 512))
+            continue;
         const double products = workgroups * 256 * blocks * blocks * depth;
         const double fixed = blocks == 1 ? 2.8 + 0.0028 * depth : 2.6 + 0.0065 * depth;
         const double busy = blocks == 1 ? 2 + 0.0085 * workgroups + 23e-9 * products : 3 + 0.001 * workgroups + 27e-9 * products;
@@ -312,16 +322,13 @@ static size_t split_bytes(Product product, int dt, int64_t T, int64_t d_in, int6
 }
 
 template <typename T_>
-static dass_status launch_product(const char *fn, Product product, int64_t d_in, int64_t d_out, const Operands<T_> &a, const Epilogue<T_> &ep,
-                                  void *workspace, hipStream_t stream)
+static dass_status launch_product(const char *fn, Product product, int64_t d_in, int64_t d_out, const Operands<T_> &a,
+                                  const Epilogue<T_> &ep, void *workspace, hipStream_t stream)
 {
     const int dt = sizeof(T_) == 2 ? DASS_BF16 : DASS_F32;
     const Plan plan = plan_of(product, dt, a.seg.rows, d_in, d_out, a.seg.n);
     if (plan.kind == Plan::kFew)
         return launch_few(fn, product, plan, a, ep, stream);
-    // 32-bit byte offsets inside a tile: 256 rows (by rows), a slab's lines (k by k)
-    if (256 * a.ldp * (int64_t)sizeof(T_) >= 0x7fffffffLL || 256 * a.ldq * (int64_t)sizeof(T_) >= 0x7fffffffLL)
-        return fail(DASS_ERR_SHAPE, "%s: rows too long for the tile addressing", fn);
     const Split split = {static_cast<float *>(workspace), output_size(product, a.seg.rows, d_in, d_out, a.seg.n), plan.splits};
     if (product == kForward)
         return launch_forward(fn, plan, a, ep, split, stream);
@@ -426,7 +433,7 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
 extern "C" size_t dass_linear_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
     using namespace dass;
-    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL ||
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > kMaxRows ||
         d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
     return split_bytes(kForward, dt, T, d_in, d_out, n_experts);
@@ -441,8 +448,9 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
     const dass_linear_task &t = *task;
     Checker c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
     c.sizes(t.T, t.d_in, t.d_out, t.n_experts, t.offsets, (int)t.dt, (int)t.act);
-    c.matrix("X", t.X, t.ldx, t.d_in, true);
-    c.matrix("W", t.W, t.ldw, t.d_in, true);
+    const int64_t read = longest_read(t.dt);
+    c.matrix("X", t.X, t.ldx, t.d_in, true, read);
+    c.matrix("W", t.W, t.ldw, t.d_in, true, read);
     c.matrix("mul", t.mul, t.ldm, t.d_out, false);
     c.matrix("residual", t.residual, t.ldr, t.d_out, false);
     c.matrix("pre_out", t.pre_out, t.ldp, t.d_out, false);
@@ -466,7 +474,8 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
 
 namespace dass {
 // What a backward call needs: g if it is kept, then the most of the bias sums and of the split products' shares.
-static size_t backward_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW, bool dbias)
+static size_t backward_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW,
+                             bool dbias)
 {
     const size_t sums = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
     const size_t x = dX ? split_bytes(kInputGrad, dt, T, d_in, d_out, n_experts) : 0;
@@ -478,7 +487,7 @@ static size_t backward_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype 
 extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
     using namespace dass;
-    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > 0x7fffffffLL ||
+    if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > kMaxRows ||
         d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
     return backward_bytes(T, d_in, d_out, dt, n_experts, true, true, true, true);
@@ -500,9 +509,10 @@ extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, v
         return fail(DASS_ERR_NULL, "%s: no gradient is asked for", fn);
     if (t.dmul && !t.mul)
         return fail(DASS_ERR_NULL, "%s: dmul without mul", fn);
-    c.matrix("dout", t.dout, t.ldg, t.d_out, true);
-    c.matrix("X", t.X, t.ldx, t.d_in, t.dW != nullptr);
-    c.matrix("W", t.W, t.ldw, t.d_in, t.dX != nullptr);
+    const int64_t read = longest_read(t.dt);
+    c.matrix("dout", t.dout, t.ldg, t.d_out, true, read);
+    c.matrix("X", t.X, t.ldx, t.d_in, t.dW != nullptr, read);
+    c.matrix("W", t.W, t.ldw, t.d_in, t.dX != nullptr, read);
     c.matrix("pre", t.pre, t.ldp, t.d_out, t.act != DASS_ACT_NONE || t.dmul);
     c.matrix("mul", t.mul, t.ldm, t.d_out, false);
     c.matrix("dX", t.dX, t.lddx, t.d_in, false);

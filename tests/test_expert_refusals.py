@@ -102,6 +102,19 @@ def test_linear_rejections(lib):
     assert lib.dass_linear_workspace_bytes(0, 64, 64, 1, 1) == lib.dass_linear_workspace_bytes(8, 64, 64, 9, 1) == 0
 
 
+def test_linear_limits(lib):
+    """What is beyond the stated sizes is refused by size alone, before any part of the work."""
+    for dt, e in ((1, 2), (0, 4)):
+        near, far = (1 << 23) // e - 16, (1 << 23) // e          # elements: rows less than 8 MiB apart, and 8 MiB
+        assert _linear(lib, dt=dt, ldx=far) == _linear(lib, dt=dt, ldw=far) == "SHAPE"
+        assert _linear(lib, dt=dt, ldx=near, ldw=near, out=ODD) == _linear(lib, dt=dt, ldo=1 << 36, out=ODD) == "ALIGN"
+        for ld in ("ldg", "ldx", "ldw"):
+            assert _grad(lib, dt=dt, **{ld: far}) == "SHAPE" and _grad(lib, dt=dt, **{ld: near}, dX=ODD) == "ALIGN"
+        assert _linear(lib, dt=dt, T=2 ** 30 + 1) == _linear(lib, dt=dt, d_out=2 ** 20 + 8, ldo=2 ** 21) == "SHAPE"
+        assert _linear(lib, dt=dt, d_in=2 ** 20 + 8, ldx=2 ** 21 - 16, ldw=2 ** 21 - 16) == "SHAPE"
+    assert lib.dass_linear_workspace_bytes(2 ** 30 + 1, 64, 64, 1, 1) == 0
+
+
 def _grad(lib, ws=A, wsb=1 << 30, **change):
     t = dict(dout=A, T=8, ldg=64, X=A, ldx=64, W=A, ldw=64, expert_stride=0, d_in=64, d_out=64, offsets=None, n_experts=1, pre=A, ldp=64,
              mul=None, ldm=0, dX=B, lddx=64, dW=C, lddw=64, dw_stride=0, dbias=None, dmul=None, lddm=0, dt=1, act=0)
