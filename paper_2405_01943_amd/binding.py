@@ -206,12 +206,13 @@ def _matrix(t: torch.Tensor, name: str):
 def _scratch(nbytes: int, device, stream=None) -> torch.Tensor:
     """A workspace for a caller that passed none.  This is a convenience of the binding (the
     library itself never allocates): the block comes from torch's caching allocator and is
-    released when the call returns, so it is tied to the stream the kernels run on; a caller
+    released when the call returns, so it is taken from the blocks of the stream the kernels run
+    on: one of another stream's could still be in use by the kernels queued there.  A caller
     that wants no allocation on its path passes ``workspace`` itself."""
-    buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
-    if stream is not None:
-        buf.record_stream(stream)   # the allocator may not hand the block on before `stream` is done with it
-    return buf
+    if stream is None:
+        return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
 
 
 # ------------------------------------------------------------------ stage 1 --
