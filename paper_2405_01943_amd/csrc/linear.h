@@ -218,9 +218,54 @@ DASS_DECLARE_TILES(launch_forward)
 DASS_DECLARE_TILES(launch_dx)
 DASS_DECLARE_TILES(launch_dw)
 #undef DASS_DECLARE_TILES
-dass_status launch_few(const char *fn, Product product, const Plan &plan, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep,
-                       hipStream_t stream);
-dass_status launch_few(const char *fn, Product product, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep,
-                       hipStream_t stream);
+// The forward product with few tiles.
+dass_status launch_few(const char *fn, const Plan &plan, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, hipStream_t stream);
+dass_status launch_few(const char *fn, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep, hipStream_t stream);
+
+// The bias sums of a gradient: db[e] = the sum of the partial sums of e's tiles of rows.
+struct BiasSums {
+    const float *partial;   // [tile number][cols]
+    int64_t cols;
+    Segments seg;
+    int tile_rows;
+    void *dbias;            // [n_experts][cols]
+};
+
+// 64 columns of one expert, in a fixed order: the workgroup's first four wavefronts take every fourth tile.
+template <typename T_>
+__device__ __forceinline__ void sum_bias(const BiasSums &b, uint32_t strip, int expert, float (*sums)[64])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Span r = segment(b.seg, expert);
+    const int64_t first = b.seg.offsets ? r.lo / b.tile_rows + expert : 0, tiles = (r.hi - r.lo + b.tile_rows - 1) / b.tile_rows;
+    const int64_t c = (int64_t)strip * 64 + lane;
+    float s = 0.0f;
+    if (c < b.cols && wave < 4) {
+#pragma unroll 8
+        for (int64_t i = wave; i < tiles; i += 4)
+            s += b.partial[(first + i) * b.cols + c];
+    }
+    if (wave < 4)
+        sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < b.cols) {
+        s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        T_ *const to = static_cast<T_ *>(b.dbias) + (int64_t)expert * b.cols + c;
+        if constexpr (sizeof(T_) == 2)
+            *to = __builtin_bit_cast(uint16_t, (__bf16)s);
+        else
+            *to = s;
+    }
+}
+
+// A gradient's parts with few tiles (f32), in one launch: dX and dW where their blocks (Plan) are not 0, the bias sums where dbias
+// is given.
+struct FewGrads {
+    Operands<float> x, w;
+    Epilogue<float> ex, ew;
+    int blocks_x, blocks_w;
+    BiasSums bias;
+};
+dass_status launch_few_grads(const char *fn, const FewGrads &grads, hipStream_t stream);
 
 }  // namespace dass

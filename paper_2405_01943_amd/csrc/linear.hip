@@ -97,32 +97,11 @@ __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout,
     }
 }
 
-// db[e] = sum of the partial sums of e's tiles, in a fixed order.  A workgroup owns 64 columns of one expert, its four
-// wavefronts every fourth tile.
 template <typename T_>
-__global__ __launch_bounds__(256) void bias_kernel(const float *__restrict__ partial, int64_t cols, Segments seg, int tile_rows,
-                                                   T_ *__restrict__ dbias)
+__global__ __launch_bounds__(256) void bias_kernel(const BiasSums b)
 {
     __shared__ float sums[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, expert = blockIdx.y;
-    const Span r = segment(seg, expert);
-    const int64_t first = seg.offsets ? r.lo / tile_rows + expert : 0, tiles = (r.hi - r.lo + tile_rows - 1) / tile_rows;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (c < cols) {
-#pragma unroll 8
-        for (int64_t i = wave; i < tiles; i += 4)
-            s += partial[(first + i) * cols + c];
-    }
-    sums[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < cols) {
-        s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-        if constexpr (sizeof(T_) == 2)
-            dbias[(int64_t)expert * cols + c] = __builtin_bit_cast(uint16_t, (__bf16)s);
-        else
-            dbias[(int64_t)expert * cols + c] = s;
-    }
+    sum_bias<T_>(b, blockIdx.x, blockIdx.y, sums);
 }
 
 // ------------------------------------------------------------------ host side --
@@ -279,7 +258,7 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
     }
     const auto one_launch = [&](int of, int threads) {   // of workgroups of `of` x `of` outputs
         const int64_t most = product == kWeightGrad ? groups * pieces(rows, of) : rows / of + groups;
-        return (double)most * pieces(cols, of) * threads < 0xffffffffu;
+        return (double)most * pieces(cols, of) * threads < 0x3fffffff;   // (a gradient's parts share one)
     };
     if (bf16 && product == kForward && share <= 8 && one_launch(16, 1024)) {
         const double bytes = 2.0 * used * cols * depth * (1 + 0.025 * (share - 1));
@@ -322,16 +301,12 @@ static size_t split_bytes(Product product, int dt, int64_t T, int64_t d_in, int6
 }
 
 template <typename T_>
-static dass_status launch_product(const char *fn, Product product, int64_t d_in, int64_t d_out, const Operands<T_> &a,
+static dass_status launch_product(const char *fn, Product product, const Plan &plan, int64_t d_in, int64_t d_out, const Operands<T_> &a,
                                   const Epilogue<T_> &ep, void *workspace, hipStream_t stream)
 {
-    const int dt = sizeof(T_) == 2 ? DASS_BF16 : DASS_F32;
-    const Plan plan = plan_of(product, dt, a.seg.rows, d_in, d_out, a.seg.n);
-    if (plan.kind == Plan::kFew)
-        return launch_few(fn, product, plan, a, ep, stream);
     const Split split = {static_cast<float *>(workspace), output_size(product, a.seg.rows, d_in, d_out, a.seg.n), plan.splits};
     if (product == kForward)
-        return launch_forward(fn, plan, a, ep, split, stream);
+        return plan.kind == Plan::kFew ? launch_few(fn, plan, a, ep, stream) : launch_forward(fn, plan, a, ep, split, stream);
     return product == kInputGrad ? launch_dx(fn, plan, a, ep, split, stream) : launch_dw(fn, plan, a, ep, split, stream);
 }
 
@@ -349,7 +324,8 @@ static dass_status run_linear(const char *fn, const dass_linear_task &t, void *w
     const Epilogue<T_> ep = {static_cast<T_ *>(t.out), t.ldo, static_cast<const T_ *>(t.bias), static_cast<const T_ *>(t.mul),
                              t.ldm, static_cast<const T_ *>(t.residual), t.ldr, static_cast<T_ *>(t.pre_out), t.ldp, t.d_out,
                              (int)t.act};
-    return launch_product(fn, kForward, t.d_in, t.d_out, a, ep, workspace, stream);
+    const Plan plan = plan_of(kForward, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
+    return launch_product(fn, kForward, plan, t.d_in, t.d_out, a, ep, workspace, stream);
 }
 
 // Whether g is a matrix of its own.
@@ -365,67 +341,72 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     int64_t ldg = t.ldg;
     // the workspace: g if it is kept, then the partial sums of the bias, whose place the split products take after them
     char *const shares = workspace + (own_g ? kept_bytes(t.T, t.d_out, t.dt) : 0);
+    const BiasSums bias = {reinterpret_cast<float *>(shares), t.d_out, seg, sum_tile_rows(t.T, t.d_out, t.dt), t.dbias};
     if (own_g || t.dbias || t.dmul) {
         T_ *kept = own_g ? reinterpret_cast<T_ *>(workspace) : nullptr;
-        float *partial = t.dbias ? reinterpret_cast<float *>(shares) : nullptr;
-        const int tile_rows = sum_tile_rows(t.T, t.d_out, t.dt);
-        const int64_t numbers = tile_numbers(seg, tile_rows), strips = (t.d_out + 64 * N - 1) / (64 * N);
+        const int64_t numbers = tile_numbers(seg, bias.tile_rows), strips = (t.d_out + 64 * N - 1) / (64 * N);
         if (numbers > 0xffffffffLL / 256 / strips)
             return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
         hipLaunchKernelGGL(slope_kernel<T_>, dim3((unsigned)(numbers * strips)), dim3(256), 0, stream,
                            static_cast<const T_ *>(t.dout), t.ldg, static_cast<const T_ *>(t.pre), t.ldp,
-                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, tile_rows, kept,
-                           static_cast<T_ *>(t.dmul), t.lddm, partial, (uint32_t)strips);
-        dass_status s = check_launch("slope kernel");
+                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, bias.tile_rows, kept,
+                           static_cast<T_ *>(t.dmul), t.lddm, t.dbias ? reinterpret_cast<float *>(shares) : nullptr, (uint32_t)strips);
+        const dass_status s = check_launch("slope kernel");
         if (s != DASS_OK)
             return s;
-        if (t.dbias) {
-            hipLaunchKernelGGL(bias_kernel<T_>, dim3((unsigned)((t.d_out + 63) / 64), (unsigned)t.n_experts), dim3(256), 0, stream,
-                               (const float *)partial, t.d_out, seg, tile_rows, static_cast<T_ *>(t.dbias));
-            s = check_launch("bias kernel");
-            if (s != DASS_OK)
-                return s;
-        }
         if (own_g) {
             g = kept;
             ldg = t.d_out;
         }
     }
-    if (t.dX) {
-        Operands<T_> a = {};
-        a.P = g;
-        a.ldp = ldg;
-        a.Q = static_cast<const T_ *>(t.W);
-        a.ldq = t.ldw;
-        a.q_stride = t.expert_stride;
-        a.depth = t.d_out;
-        a.seg = seg;
-        Epilogue<T_> ep = {};
-        ep.out = static_cast<T_ *>(t.dX);
-        ep.ldo = t.lddx;
-        ep.cols = t.d_in;
-        ep.act = DASS_ACT_NONE;
-        const dass_status s = launch_product(fn, kInputGrad, t.d_in, t.d_out, a, ep, shares, stream);
+
+    Operands<T_> ax = {}, aw = {};
+    Epilogue<T_> ex = {}, ew = {};
+    ax.P = aw.P = g;
+    ax.ldp = aw.ldp = ldg;
+    ax.seg = aw.seg = seg;
+    ex.cols = ew.cols = t.d_in;
+    ex.act = ew.act = DASS_ACT_NONE;
+    ax.Q = static_cast<const T_ *>(t.W);
+    ax.ldq = t.ldw;
+    ax.q_stride = t.expert_stride;
+    ax.depth = t.d_out;
+    ex.out = static_cast<T_ *>(t.dX);
+    ex.ldo = t.lddx;
+    aw.Q = static_cast<const T_ *>(t.X);
+    aw.ldq = t.ldx;
+    aw.out_stride = t.dw_stride;
+    aw.out_rows = t.d_out;
+    ew.out = static_cast<T_ *>(t.dW);
+    ew.ldo = t.lddw;
+    const Plan px = plan_of(kInputGrad, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
+    const Plan pw = plan_of(kWeightGrad, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
+    const bool few_x = t.dX && px.kind == Plan::kFew, few_w = t.dW && pw.kind == Plan::kFew;
+    const bool tiles_x = t.dX && !few_x, tiles_w = t.dW && !few_w;
+    // with the few tiles of the products, if no split product takes the partial sums' place
+    const bool bias_with_few = (few_x || few_w) && !tiles_x && !tiles_w && (t.d_out + 63) / 64 * t.n_experts <= 1 << 20;
+    if (t.dbias && !bias_with_few) {
+        hipLaunchKernelGGL(bias_kernel<T_>, dim3((unsigned)((t.d_out + 63) / 64), (unsigned)t.n_experts), dim3(256), 0, stream, bias);
+        const dass_status s = check_launch("bias kernel");
         if (s != DASS_OK)
             return s;
     }
-    if (t.dW) {
-        Operands<T_> a = {};
-        a.P = g;
-        a.ldp = ldg;
-        a.Q = static_cast<const T_ *>(t.X);
-        a.ldq = t.ldx;
-        a.out_stride = t.dw_stride;
-        a.out_rows = t.d_out;
-        a.seg = seg;
-        Epilogue<T_> ep = {};
-        ep.out = static_cast<T_ *>(t.dW);
-        ep.ldo = t.lddw;
-        ep.cols = t.d_in;
-        ep.act = DASS_ACT_NONE;
-        return launch_product(fn, kWeightGrad, t.d_in, t.d_out, a, ep, shares, stream);
+    if constexpr (sizeof(T_) == 4) {
+        if (few_x || few_w) {
+            FewGrads few = {ax, aw, ex, ew, few_x ? px.blocks : 0, few_w ? pw.blocks : 0, bias};
+            if (!bias_with_few)
+                few.bias.dbias = nullptr;
+            const dass_status s = launch_few_grads(fn, few, stream);
+            if (s != DASS_OK)
+                return s;
+        }
     }
-    return DASS_OK;
+    if (tiles_x) {
+        const dass_status s = launch_product(fn, kInputGrad, px, t.d_in, t.d_out, ax, ex, shares, stream);
+        if (s != DASS_OK)
+            return s;
+    }
+    return tiles_w ? launch_product(fn, kWeightGrad, pw, t.d_in, t.d_out, aw, ew, shares, stream) : DASS_OK;
 }
 
 }  // namespace dass

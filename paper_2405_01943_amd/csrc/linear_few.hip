@@ -1,4 +1,6 @@
-// Products with few output tiles: the forward product of few rows (bf16, f32) and small f32 products of every kind.
+// Products with few output tiles: the forward product of few rows (bf16, f32) and small f32 products of every kind.  A gradient's
+// two products and its bias sums are parts of one launch, as none needs another's result: a gradient of 301 rows of 256 x 688 with
+// its bias 12.1 us in graphs, 19.6 with three launches (7.7, 5.3 and 2.6 us of them), of 1024 rows of 512 x 512 22.5 and 28.5.
 //
 // A workgroup owns 16 TB rows x 16 CB columns of the output and its WAVES wavefronts split k between them, so that a
 // grid of few tiles still has loads on their way in every compute unit; the partial sums meet in LDS once.  Fragments
@@ -35,19 +37,18 @@ struct Few<float> {
     }
 };
 
+// One workgroup's tile; `expert` is given for dW and found for the others.
 template <typename T_, Product PRODUCT, int TB, int CB, int WAVES, int PAIRS>
-__global__ __launch_bounds__(64 * WAVES) void product_few_kernel(const Operands<T_> a, const Epilogue<T_> ep, uint32_t tiles_c)
+__device__ __forceinline__ void few_tile(const Operands<T_> &a, const Epilogue<T_> &ep, uint32_t tile_r, uint32_t tile_c, int expert,
+                                         f32x4 *lds)
 {
     typedef Few<T_> F;
     constexpr bool P_ROWS = PRODUCT != kWeightGrad, Q_ROWS = PRODUCT == kForward;   // stored row by row
     static_assert(PRODUCT == kForward || sizeof(T_) == 4, "k by k in f32 only");
     const int lane = threadIdx.x & 63, fr = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x - tile_r * tiles_c;
-    int expert;
     int64_t r0, r_end, k0 = 0, k_end = a.depth;
     if constexpr (PRODUCT == kWeightGrad) {
-        expert = blockIdx.y;
         const Span k = segment(a.seg, expert);
         k0 = k.lo;
         k_end = k.hi;
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(const Operands<
     }
 
     // The partial sums meet: a thread adds up four neighbouring columns of one row, in the order of the wavefronts.
-    __shared__ f32x4 sums[WAVES][CB * TB][64];
+    auto sums = reinterpret_cast<f32x4(*)[CB * TB][64]>(lds);   // [WAVES]
 #pragma unroll
     for (int i = 0; i < CB; ++i)
 #pragma unroll
@@ -142,45 +143,100 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(const Operands<
     }
 }
 
-template <typename T_, Product PRODUCT, int TB, int CB, int WAVES, int PAIRS>
-static dass_status launch(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, hipStream_t stream)
+// Wavefronts of a workgroup in f32, with the loads that each has on its way where the blocks are small.  8 against 4 with twice the
+// loads: 16 rows of 1024 x 1024 5.7 and 6.9 us, 301 of 256 x 688 (blocks of 32) 4.7 and 5.2.  16 read no more at a time and have
+// more sums to add: the gradient of 16 rows of 1024 x 1024 10.5 us, with 16 13.2 (100 of 64 x 4096 23.9 and 18.6).
+constexpr int kFewWaves = 8;
+static constexpr int few_pairs(int blocks) { return 2 / blocks; }
+
+template <typename T_, int BLOCKS, int WAVES, int PAIRS>
+__global__ __launch_bounds__(64 * WAVES) void few_forward_kernel(const Operands<T_> a, const Epilogue<T_> ep, uint32_t tiles_c)
 {
-    const int64_t tiles_r = PRODUCT == kWeightGrad ? (a.out_rows + 16 * TB - 1) / (16 * TB) : tile_numbers(a.seg, 16 * TB);
-    const int64_t tiles_c = (ep.cols + 16 * CB - 1) / (16 * CB);
-    const unsigned experts = PRODUCT == kWeightGrad ? a.seg.n : 1;
-    if (tiles_r > 0xffffffffLL / (64 * WAVES) / tiles_c / experts)
+    __shared__ f32x4 lds[WAVES * BLOCKS * BLOCKS * 64];
+    const uint32_t tile_r = blockIdx.x / tiles_c;
+    few_tile<T_, kForward, BLOCKS, BLOCKS, WAVES, PAIRS>(a, ep, tile_r, blockIdx.x - tile_r * tiles_c, 0, lds);
+}
+
+// Workgroups 0 .. x - 1 dX's, the next w dW's, expert by expert, the rest the bias sums'.
+struct FewParts {
+    uint32_t x, x_cols, w, w_rows, w_cols, bias_strips;
+};
+
+template <int BX, int BW>
+__global__ __launch_bounds__(64 * kFewWaves) void few_grad_kernel(const Operands<float> ax, const Epilogue<float> ex,
+                                                                  const Operands<float> aw, const Epilogue<float> ew, const BiasSums bias,
+                                                                  const FewParts parts)
+{
+    constexpr int MOST = BX > BW ? BX : BW;
+    __shared__ f32x4 lds[kFewWaves * MOST * MOST * 64];
+    uint32_t i = blockIdx.x;
+    if (i < parts.x) {
+        const uint32_t tile_r = i / parts.x_cols;
+        few_tile<float, kInputGrad, BX, BX, kFewWaves, few_pairs(BX)>(ax, ex, tile_r, i - tile_r * parts.x_cols, 0, lds);
+        return;
+    }
+    i -= parts.x;
+    if (i < parts.w) {
+        const uint32_t line = i / parts.w_cols, expert = line / parts.w_rows;
+        few_tile<float, kWeightGrad, BW, BW, kFewWaves, few_pairs(BW)>(aw, ew, line - expert * parts.w_rows, i - line * parts.w_cols,
+                                                                       expert, lds);
+        return;
+    }
+    i -= parts.w;
+    const uint32_t expert = i / parts.bias_strips;
+    sum_bias<float>(bias, i - expert * parts.bias_strips, expert, reinterpret_cast<float(*)[64]>(lds));
+}
+
+template <typename T_, int BLOCKS, int WAVES, int PAIRS>
+static dass_status launch_rows(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, hipStream_t stream)
+{
+    const int64_t tiles_r = tile_numbers(a.seg, 16 * BLOCKS), tiles_c = (ep.cols + 16 * BLOCKS - 1) / (16 * BLOCKS);
+    if (tiles_r > 0xffffffffLL / (64 * WAVES) / tiles_c)
         return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
-    hipLaunchKernelGGL((product_few_kernel<T_, PRODUCT, TB, CB, WAVES, PAIRS>), dim3((unsigned)(tiles_r * tiles_c), experts),
-                       dim3(64 * WAVES), 0, stream, a, ep, (uint32_t)tiles_c);
+    hipLaunchKernelGGL((few_forward_kernel<T_, BLOCKS, WAVES, PAIRS>), dim3((unsigned)(tiles_r * tiles_c)), dim3(64 * WAVES), 0, stream, a,
+                       ep, (uint32_t)tiles_c);
     return check_launch("few-tile product kernel");
 }
 
-// Wavefronts of a workgroup and loads that each has on its way, in graphs: one row of 4096 x 11008 4 wavefronts x 8 fragments 20.0 us, 8
-// x 4 19.1, 16 x 4 17.7; of 4096 x 4096 9.4, 8.8, 8.3; but of 1024 x 4096 4.0 (x 4 3.9), 4.0, 5.1, four rows of 512 x 512 3.4 (x 4
-// 2.8), 3.4, 3.6.
-dass_status launch_few(const char *fn, Product, const Plan &, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, hipStream_t stream)
+// Wavefronts of a workgroup and loads that each has on its way, in graphs: one row of 4096 x 11008 4 wavefronts x 8 fragments 20.0
+// us, 8 x 4 19.1, 16 x 4 17.7; of 4096 x 4096 9.4, 8.8, 8.3; but of 1024 x 4096 4.0 (x 4 3.9), 4.0, 5.1, four rows of 512 x 512
+// 3.4 (x 4 2.8), 3.4, 3.6.
+dass_status launch_few(const char *fn, const Plan &, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, hipStream_t stream)
 {
     if (a.depth >= 4096)
-        return launch<uint16_t, kForward, 1, 1, 16, 2>(fn, a, ep, stream);
-    return launch<uint16_t, kForward, 1, 1, 4, 2>(fn, a, ep, stream);
+        return launch_rows<uint16_t, 1, 16, 2>(fn, a, ep, stream);
+    return launch_rows<uint16_t, 1, 4, 2>(fn, a, ep, stream);
 }
 
-// The same in f32, 8 wavefronts against 4 with twice the loads: 16 rows of 1024 x 1024 5.7 and 6.9 us, 301 of 256 x 688 (blocks of 32) 4.7
-// and 5.2, its dX 7.7 and 9.1, dW 5.3 and 6.6.
-template <int BLOCKS>
-static dass_status launch_blocks(const char *fn, Product product, const Operands<float> &a, const Epilogue<float> &ep, hipStream_t stream)
+dass_status launch_few(const char *fn, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep, hipStream_t stream)
 {
-    if (product == kForward)
-        return launch<float, kForward, BLOCKS, BLOCKS, 8, 2 / BLOCKS>(fn, a, ep, stream);
-    if (product == kInputGrad)
-        return launch<float, kInputGrad, BLOCKS, BLOCKS, 8, 2 / BLOCKS>(fn, a, ep, stream);
-    return launch<float, kWeightGrad, BLOCKS, BLOCKS, 8, 2 / BLOCKS>(fn, a, ep, stream);
+    if (plan.blocks == 1)
+        return launch_rows<float, 1, kFewWaves, few_pairs(1)>(fn, a, ep, stream);
+    return launch_rows<float, 2, kFewWaves, few_pairs(2)>(fn, a, ep, stream);
 }
 
-dass_status launch_few(const char *fn, Product product, const Plan &plan, const Operands<float> &a, const Epilogue<float> &ep,
-                       hipStream_t stream)
+template <int BX, int BW>
+static dass_status launch_grads(const char *fn, const FewGrads &f, hipStream_t stream)
 {
-    return plan.blocks == 1 ? launch_blocks<1>(fn, product, a, ep, stream) : launch_blocks<2>(fn, product, a, ep, stream);
+    const auto pieces = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
+    const int64_t x_cols = pieces(f.ex.cols, 16 * BX), x = f.blocks_x ? tile_numbers(f.x.seg, 16 * BX) * x_cols : 0;
+    const int64_t w_rows = pieces(f.w.out_rows, 16 * BW), w_cols = pieces(f.ew.cols, 16 * BW);
+    const int64_t w = f.blocks_w ? w_rows * w_cols * f.w.seg.n : 0;
+    const int64_t strips = pieces(f.bias.cols, 64), bias = f.bias.dbias ? strips * f.bias.seg.n : 0;
+    if (x + w + bias > 0xffffffffLL / (64 * kFewWaves))
+        return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
+    const FewParts parts = {(uint32_t)x, (uint32_t)x_cols, (uint32_t)w, (uint32_t)w_rows, (uint32_t)w_cols, (uint32_t)strips};
+    hipLaunchKernelGGL((few_grad_kernel<BX, BW>), dim3((unsigned)(x + w + bias)), dim3(64 * kFewWaves), 0, stream, f.x, f.ex, f.w, f.ew,
+                       f.bias, parts);
+    return check_launch("few-tile gradient kernel");
+}
+
+dass_status launch_few_grads(const char *fn, const FewGrads &f, hipStream_t stream)
+{
+    const int bx = f.blocks_x ? f.blocks_x : f.blocks_w, bw = f.blocks_w ? f.blocks_w : f.blocks_x;
+    if (bx == 1)
+        return bw == 1 ? launch_grads<1, 1>(fn, f, stream) : launch_grads<1, 2>(fn, f, stream);
+    return bw == 1 ? launch_grads<2, 1>(fn, f, stream) : launch_grads<2, 2>(fn, f, stream);
 }
 
 }  // namespace dass
