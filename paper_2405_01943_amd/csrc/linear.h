@@ -206,6 +206,7 @@ struct Plan {
     int tile;     // kTiles: 0: 256 x 256, 1: 128 x 256, 2: 128 x 128 (f32: always 2), 3: 128 x 128, two a compute unit
     int splits;   // kTiles: shares of k
     int blocks;   // kFew: 16-row (and in f32 16-column) blocks of a workgroup
+    double us;    // the estimate, where it is one of several launches to choose from
 };
 
 // One launch each, two with split k; errors as the entry points report them.
@@ -267,5 +268,9 @@ struct FewGrads {
     BiasSums bias;
 };
 dass_status launch_few_grads(const char *fn, const FewGrads &grads, hipStream_t stream);
+
+// The same for both products with 128 x 128 tiles, none of them split (bf16); the bias sums where dbias is given.
+dass_status launch_pair(const char *fn, bool short_tiles, const Operands<uint16_t> &ax, const Epilogue<uint16_t> &ex,
+                        const Operands<uint16_t> &aw, const Epilogue<uint16_t> &ew, const BiasSums &bias, hipStream_t stream);
 
 }  // namespace dass

@@ -193,6 +193,30 @@ struct Checker {
     }
 };
 
+static int64_t pieces(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+// The tiles of a product in the direction of its rows; experts of uneven size have half a tile more each.
+static int64_t row_tiles(Product product, int64_t groups, int64_t rows, int64_t of)
+{
+    if (product == kWeightGrad || groups == 1)
+        return groups * pieces(rows, of);
+    const int64_t used = std::min(groups, rows);
+    return std::max(used, rows / of + used / 2);
+}
+
+struct Tile {
+    int rows, cols, slots;   // slots: workgroups that the card holds
+    double start, slab;      // us of a workgroup and of each slab of k
+    // alone on its compute unit a workgroup of the short tile is not held up by a second
+    double time(int64_t slabs, int64_t tiles) const
+    {
+        return slots == 512 && tiles <= 256 ? 4.47 + slabs * 0.689 : start + slabs * slab;
+    }
+};
+static const Tile kTiles[] = {{256, 256, 256, 8.8, 1.34}, {128, 256, 256, 5.4, 0.87}, {128, 128, 256, 4.06, 0.517},
+                              {128, 128, 512, 3.47, 0.985}},
+                  kTileF32 = {128, 128, 256, 3.4, 2.49};
+
 // The kernel, the tile and the split of k that are expected to be fastest for the products of `groups` experts: cols columns,
 // `depth` of k each, and `rows` rows each (dW) or all together.  The estimates, in us, are fitted to times of 149 bf16 and 45
 // f32 products of 1 to 16384 rows and every tile with 1 to 16 shares; over the bf16 ones the choice is 1 % slower than the best
@@ -217,42 +241,27 @@ struct Checker {
 static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, int64_t cols, int64_t depth)
 {
     const bool bf16 = dt == DASS_BF16;
-    const auto pieces = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
     const int64_t share = product == kWeightGrad ? rows : pieces(rows, groups);   // of an expert, were they even
     const int64_t used = std::min(groups, rows);
-    // the row tiles of experts of uneven size: half a tile more each
-    const auto row_tiles = [&](int64_t of) {
-        if (product == kWeightGrad || groups == 1)
-            return groups * pieces(rows, of);
-        return std::max(used, rows / of + used / 2);
-    };
-
     static const int kShares[] = {1, 2, 3, 4, 6, 8, 12, 16};
-    static const struct {
-        int rows, cols, slots;   // slots: workgroups that the card holds
-        double start, slab;
-    } kTiles[] = {{256, 256, 256, 8.8, 1.34}, {128, 256, 256, 5.4, 0.87}, {128, 128, 256, 4.06, 0.517}, {128, 128, 512, 3.47, 0.985}},
-      kTileF32 = {128, 128, 256, 3.4, 2.49};
     const double join = bf16 ? 3.64 : 2.4, byte = bf16 ? 1 / 6.13e6 : 1 / 4.5e6;   // us, us a byte
     const int64_t slabs = pieces(depth, bf16 ? 64 : 32), outputs = (product == kWeightGrad ? groups : 1) * rows * cols;
     const double weights = product == kWeightGrad ? 0 : (bf16 ? 6 : 0) + (bf16 ? 2.0 / 5.2e6 : 4.0 / 4.6e6) * used * cols * depth;
     const double written = bf16 ? 2.0 / 3.38e6 * outputs : 0;
-    Plan best = {Plan::kTiles, bf16 ? 0 : 2, 1, 0};
+    Plan best = {Plan::kTiles, bf16 ? 0 : 2, 1, 0, 0};
     double best_time = 1e300;
     for (int k = bf16 ? 0 : 2; k < (bf16 ? 4 : 3); ++k) {
-        const auto &t = bf16 ? kTiles[k] : kTileF32;
-        const int64_t tiles = row_tiles(t.rows) * pieces(cols, t.cols);
+        const Tile &t = bf16 ? kTiles[k] : kTileF32;
+        const int64_t tiles = row_tiles(product, groups, rows, t.rows) * pieces(cols, t.cols);
         for (const int z : kShares) {
             if (z > 1 && (k == 3 || slabs < 2 * z || (double)z * outputs * 4 > 256e6))
                 break;
-            // alone on its compute unit a workgroup of the short tile is not held up by a second
-            const double one = k == 3 && tiles <= 256 ? 4.47 + slabs * 0.689 : t.start + pieces(slabs, z) * t.slab;
-            const double busy = pieces(tiles * z, t.slots) * one, memory = weights + (z == 1 ? written : 0);
+            const double busy = pieces(tiles * z, t.slots) * t.time(pieces(slabs, z), tiles), memory = weights + (z == 1 ? written : 0);
             const double time = std::max(busy, memory) + (bf16 ? 0.093 * std::min(busy, memory) : 0) +
                                 (z > 1 ? join + z * 8.0 * outputs * byte : 0);
             if (time < best_time) {
                 best_time = time;
-                best = {Plan::kTiles, k, z, 0};
+                best = {Plan::kTiles, k, z, 0, time};
             }
         }
     }
@@ -263,10 +272,10 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
     if (bf16 && product == kForward && share <= 8 && one_launch(16, 1024)) {
         const double bytes = 2.0 * used * cols * depth * (1 + 0.025 * (share - 1));
         if ((share == 1 && groups > 1) || std::max(2 + 0.0011 * depth, 2 + bytes / 5.1e6) < best_time)
-            return {Plan::kFew, 0, 1, 1};
+            return {Plan::kFew, 0, 1, 1, 0};
     }
     for (int blocks = 1; !bf16 && blocks <= 2; ++blocks) {
-        const double workgroups = (double)row_tiles(16 * blocks) * pieces(cols, 16 * blocks);
+        const double workgroups = (double)row_tiles(product, groups, rows, 16 * blocks) * pieces(cols, 16 * blocks);
         if (!one_launch(16 * blocks, 512))
             continue;
         const double products = workgroups * 256 * blocks * blocks * depth;
@@ -274,7 +283,7 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
         const double busy = blocks == 1 ? 2 + 0.0085 * workgroups + 23e-9 * products : 3 + 0.001 * workgroups + 27e-9 * products;
         if (fixed < best_time && busy < best_time) {
             best_time = std::max(fixed, busy);
-            best = {Plan::kFew, 0, 1, blocks};
+            best = {Plan::kFew, 0, 1, blocks, best_time};
         }
     }
     return best;
@@ -289,15 +298,68 @@ static Plan plan_of(Product product, int dt, int64_t T, int64_t d_in, int64_t d_
     return plan_product(product, dt, n_experts, d_out, d_in, (T + n_experts - 1) / n_experts);
 }
 
+// Whether both products of a bf16 gradient (and its bias sums) go into one launch, with 128 x 128 tiles (2), short ones (3) or not
+// at all (0): beside each other the tiles of two small products take as long as the longer one, or beyond one round their work
+// over the slots and half a tile.  In graphs, with the element-wise pass and bias sums: 301 rows of 256 x 688 22.0 us, in one launch
+// 13.1; 1030 of 576 x 520 29.4, 18.2; 1024 of 2048 x 2048 44.1, 32.7; 2000 rows over 8 experts of 512 x 1024 35.3, 22.9;
+// but 512 of 1024 x 4096 34.0, 43.1, where each alone fills the chip, and 16384 of 512 x 512 57.5, 170.8, where k has to be split.  Over 50
+// sizes the choice is 1 % slower than the best in the mean, and 1.29 times as fast as two launches always.
+static int pair_of(const Plan &x, const Plan &w, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+{
+    const int64_t tiles_x = row_tiles(kInputGrad, n_experts, T, 128) * pieces(d_in, 128);
+    const int64_t tiles_w = n_experts * pieces(d_out, 128) * pieces(d_in, 128), tiles = tiles_x + tiles_w;
+    if (tiles > 1 << 20)
+        return 0;
+    const int64_t slabs_x = pieces(d_out, 64), slabs_w = pieces(pieces(T, n_experts), 64);
+    const double memory = 6 + 2.0 / 5.2e6 * std::min(n_experts, T) * d_in * d_out + 2.0 / 3.38e6 * ((double)T + n_experts * d_out) * d_in;
+    int best = 0;
+    double best_time = x.us + w.us + 2;   // 2: the second launch
+    for (int k = 2; k <= 3; ++k) {
+        const double one_x = kTiles[k].time(slabs_x, tiles), one_w = kTiles[k].time(slabs_w, tiles), longer = std::max(one_x, one_w);
+        const double busy = tiles <= kTiles[k].slots ? longer : (tiles_x * one_x + tiles_w * one_w) / kTiles[k].slots + longer / 2;
+        const double time = std::max(busy, memory);
+        if (time < best_time) {
+            best_time = time;
+            best = k;
+        }
+    }
+    return best;
+}
+
 static int64_t output_size(Product product, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
 {
     return product == kForward ? T * d_out : product == kInputGrad ? T * d_in : n_experts * d_out * d_in;
 }
 
-static size_t split_bytes(Product product, int dt, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+static size_t split_bytes(const Plan &plan, Product product, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
 {
-    const Plan plan = plan_of(product, dt, T, d_in, d_out, n_experts);
     return plan.splits > 1 ? round_up((size_t)plan.splits * output_size(product, T, d_in, d_out, n_experts) * 4, 256) : 0;
+}
+
+// What a gradient's call takes and needs: g if it is kept, then the most of the bias sums and of the split products' shares.
+struct GradPlan {
+    Plan x, w;
+    int pair;
+    size_t bytes;
+};
+
+static GradPlan plan_grad(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW,
+                          bool dbias)
+{
+    GradPlan p = {};
+    if (dX)
+        p.x = plan_of(kInputGrad, dt, T, d_in, d_out, n_experts);
+    if (dW)
+        p.w = plan_of(kWeightGrad, dt, T, d_in, d_out, n_experts);
+    if (dX && dW && dt == DASS_BF16)
+        p.pair = pair_of(p.x, p.w, T, d_in, d_out, n_experts);
+    p.bytes = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
+    if (dX && !p.pair)
+        p.bytes = std::max(p.bytes, split_bytes(p.x, kInputGrad, T, d_in, d_out, n_experts));
+    if (dW && !p.pair)
+        p.bytes = std::max(p.bytes, split_bytes(p.w, kWeightGrad, T, d_in, d_out, n_experts));
+    p.bytes += keeps_g ? kept_bytes(T, d_out, dt) : 0;
+    return p;
 }
 
 template <typename T_>
@@ -311,7 +373,7 @@ static dass_status launch_product(const char *fn, Product product, const Plan &p
 }
 
 template <typename T_>
-static dass_status run_linear(const char *fn, const dass_linear_task &t, void *workspace, hipStream_t stream)
+static dass_status run_linear(const char *fn, const dass_linear_task &t, const Plan &plan, void *workspace, hipStream_t stream)
 {
     Operands<T_> a = {};
     a.P = static_cast<const T_ *>(t.X);
@@ -324,7 +386,6 @@ static dass_status run_linear(const char *fn, const dass_linear_task &t, void *w
     const Epilogue<T_> ep = {static_cast<T_ *>(t.out), t.ldo, static_cast<const T_ *>(t.bias), static_cast<const T_ *>(t.mul),
                              t.ldm, static_cast<const T_ *>(t.residual), t.ldr, static_cast<T_ *>(t.pre_out), t.ldp, t.d_out,
                              (int)t.act};
-    const Plan plan = plan_of(kForward, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
     return launch_product(fn, kForward, plan, t.d_in, t.d_out, a, ep, workspace, stream);
 }
 
@@ -332,7 +393,8 @@ static dass_status run_linear(const char *fn, const dass_linear_task &t, void *w
 static bool keeps_g(const dass_linear_grad_task &t) { return (t.act != DASS_ACT_NONE || t.mul) && (t.dX || t.dW); }
 
 template <typename T_>
-static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &t, char *workspace, hipStream_t stream)
+static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &t, const GradPlan &plan, char *workspace,
+                                   hipStream_t stream)
 {
     constexpr int N = Chunk<T_>::N;
     const Segments seg = {t.offsets, t.T, (int)t.n_experts};
@@ -379,12 +441,14 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     aw.out_rows = t.d_out;
     ew.out = static_cast<T_ *>(t.dW);
     ew.ldo = t.lddw;
-    const Plan px = plan_of(kInputGrad, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
-    const Plan pw = plan_of(kWeightGrad, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
-    const bool few_x = t.dX && px.kind == Plan::kFew, few_w = t.dW && pw.kind == Plan::kFew;
+    const bool few_x = t.dX && plan.x.kind == Plan::kFew, few_w = t.dW && plan.w.kind == Plan::kFew;
     const bool tiles_x = t.dX && !few_x, tiles_w = t.dW && !few_w;
     // with the few tiles of the products, if no split product takes the partial sums' place
     const bool bias_with_few = (few_x || few_w) && !tiles_x && !tiles_w && (t.d_out + 63) / 64 * t.n_experts <= 1 << 20;
+    if constexpr (sizeof(T_) == 2) {
+        if (plan.pair)
+            return launch_pair(fn, plan.pair == 3, ax, ex, aw, ew, bias, stream);
+    }
     if (t.dbias && !bias_with_few) {
         hipLaunchKernelGGL(bias_kernel<T_>, dim3((unsigned)((t.d_out + 63) / 64), (unsigned)t.n_experts), dim3(256), 0, stream, bias);
         const dass_status s = check_launch("bias kernel");
@@ -393,7 +457,7 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     }
     if constexpr (sizeof(T_) == 4) {
         if (few_x || few_w) {
-            FewGrads few = {ax, aw, ex, ew, few_x ? px.blocks : 0, few_w ? pw.blocks : 0, bias};
+            FewGrads few = {ax, aw, ex, ew, few_x ? plan.x.blocks : 0, few_w ? plan.w.blocks : 0, bias};
             if (!bias_with_few)
                 few.bias.dbias = nullptr;
             const dass_status s = launch_few_grads(fn, few, stream);
@@ -402,11 +466,11 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
         }
     }
     if (tiles_x) {
-        const dass_status s = launch_product(fn, kInputGrad, px, t.d_in, t.d_out, ax, ex, shares, stream);
+        const dass_status s = launch_product(fn, kInputGrad, plan.x, t.d_in, t.d_out, ax, ex, shares, stream);
         if (s != DASS_OK)
             return s;
     }
-    return tiles_w ? launch_product(fn, kWeightGrad, pw, t.d_in, t.d_out, aw, ew, shares, stream) : DASS_OK;
+    return tiles_w ? launch_product(fn, kWeightGrad, plan.w, t.d_in, t.d_out, aw, ew, shares, stream) : DASS_OK;
 }
 
 }  // namespace dass
@@ -417,7 +481,7 @@ extern "C" size_t dass_linear_workspace_bytes(int64_t T, int64_t d_in, int64_t d
     if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > kMaxRows ||
         d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
-    return split_bytes(kForward, dt, T, d_in, d_out, n_experts);
+    return split_bytes(plan_of(kForward, dt, T, d_in, d_out, n_experts), kForward, T, d_in, d_out, n_experts);
 }
 
 extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace, size_t workspace_bytes, void *hip_stream)
@@ -444,26 +508,15 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
         c.apart("out", t.out, {t.out});
     if (c.status != DASS_OK)
         return c.status;
-    const size_t need = dass_linear_workspace_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts);
+    const Plan plan = plan_of(kForward, t.dt, t.T, t.d_in, t.d_out, t.n_experts);
+    const size_t need = split_bytes(plan, kForward, t.T, t.d_in, t.d_out, t.n_experts);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(DASS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
     if (need > 0 && !aligned16(workspace))
         return fail(DASS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", fn);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return t.dt == DASS_BF16 ? run_linear<uint16_t>(fn, t, workspace, stream) : run_linear<float>(fn, t, workspace, stream);
+    return t.dt == DASS_BF16 ? run_linear<uint16_t>(fn, t, plan, workspace, stream) : run_linear<float>(fn, t, plan, workspace, stream);
 }
-
-namespace dass {
-// What a backward call needs: g if it is kept, then the most of the bias sums and of the split products' shares.
-static size_t backward_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW,
-                             bool dbias)
-{
-    const size_t sums = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
-    const size_t x = dX ? split_bytes(kInputGrad, dt, T, d_in, d_out, n_experts) : 0;
-    const size_t w = dW ? split_bytes(kWeightGrad, dt, T, d_in, d_out, n_experts) : 0;
-    return (keeps_g ? kept_bytes(T, d_out, dt) : 0) + std::max(sums, std::max(x, w));
-}
-}  // namespace dass
 
 extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts)
 {
@@ -471,7 +524,10 @@ extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, 
     if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > kMaxRows ||
         d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
-    return backward_bytes(T, d_in, d_out, dt, n_experts, true, true, true, true);
+    // the most that a call of all or some of the gradients needs: one alone may be split where both together are not
+    return std::max(plan_grad(T, d_in, d_out, dt, n_experts, true, true, false, true).bytes,
+                    std::max(plan_grad(T, d_in, d_out, dt, n_experts, true, false, true, true).bytes,
+                             plan_grad(T, d_in, d_out, dt, n_experts, true, true, true, true).bytes));
 }
 
 extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, void *workspace, size_t workspace_bytes,
@@ -515,12 +571,13 @@ extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, v
         c.stride("dW", t.dw_stride, t.lddw, t.d_in, t.d_out, t.n_experts);
     if (c.status != DASS_OK)
         return c.status;
-    const size_t need = backward_bytes(t.T, t.d_in, t.d_out, t.dt, t.n_experts, keeps_g(t), t.dX, t.dW, t.dbias);
+    const GradPlan plan = plan_grad(t.T, t.d_in, t.d_out, t.dt, t.n_experts, keeps_g(t), t.dX, t.dW, t.dbias);
+    const size_t need = plan.bytes;
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(DASS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
     if (need > 0 && !aligned16(workspace))
         return fail(DASS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", fn);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char *ws = static_cast<char *>(workspace);
-    return t.dt == DASS_BF16 ? run_linear_grad<uint16_t>(fn, t, ws, stream) : run_linear_grad<float>(fn, t, ws, stream);
+    return t.dt == DASS_BF16 ? run_linear_grad<uint16_t>(fn, t, plan, ws, stream) : run_linear_grad<float>(fn, t, plan, ws, stream);
 }

@@ -320,8 +320,10 @@ __device__ __forceinline__ TileOrder order_runs(uint32_t tiles_r, uint32_t tiles
 
 // SHORT: rings of two parts each, 64 KB in all, so that two workgroups share a compute unit and one's loads and stores go on
 // beside the other's products: for k of few slabs.
+// `block` is a place in the tile order, `nth` the share of k, `expert` is given for dW and found for the others.
 template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT>
-__global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a, const Epilogue<T_> ep0, const TileOrder order, const Split split)
+__device__ __forceinline__ void product_tile(const Operands<T_> &a, const Epilogue<T_> &ep0, const TileOrder &order, const Split &split,
+                                             uint32_t block, int expert, uint32_t nth)
 {
     constexpr bool BY_HAND = sizeof(T_) == 2 && PRODUCT != kForward;   // transposing reads
     typedef Part<T_, PRODUCT != kWeightGrad, RB, BY_HAND> PartP;
@@ -341,15 +343,13 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     extern __shared__ __attribute__((aligned(1024))) char lds[];   // LDS bytes
 
     uint32_t tile_r, tile_c;   // tile_order.h
-    int expert = 0;
     int64_t r0, r_end, k0 = 0, depth = a.depth;
     if (PRODUCT == kWeightGrad || !a.seg.offsets) {
-        if (!tile_of_block(order, blockIdx.x, tile_r, tile_c))
+        if (!tile_of_block(order, block, tile_r, tile_c))
             return;
         r0 = (int64_t)tile_r * BR;
         r_end = PRODUCT == kWeightGrad ? a.out_rows : a.seg.rows;
         if constexpr (PRODUCT == kWeightGrad) {
-            expert = blockIdx.y;
             const Span k = segment(a.seg, expert);
             k0 = k.lo;
             depth = k.hi - k.lo;
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     } else {   // the order for the tiles that there are: runs
         const TileList list(a.seg, BR);
         const TileOrder runs = order_runs(list.total, order.tiles_n, BR < BC ? 8 : kPatchT);
-        if (list.total == 0 || blockIdx.x / kXcds >= runs.per_xcd || !tile_of_block(runs, blockIdx.x, tile_r, tile_c))
+        if (list.total == 0 || block / kXcds >= runs.per_xcd || !tile_of_block(runs, block, tile_r, tile_c))
             return;
         const Span r = list.rows(a.seg, BR, (int)tile_r, expert);
         r0 = r.lo;
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     if (split.n > 1) {   // this workgroup's share of the slabs, perhaps none
-        const int64_t share = ((depth + SLAB - 1) / SLAB + split.n - 1) / split.n * SLAB, from = share * blockIdx.z;
+        const int64_t share = ((depth + SLAB - 1) / SLAB + split.n - 1) / split.n * SLAB, from = share * nth;
         depth = from >= depth ? 0 : depth - from < share ? depth - from : share;
         k0 += from;
     }
@@ -596,7 +596,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     const int fr = lane & 15, g = lane >> 4;
     int64_t row = r0 + wr * 16 * RB + lane / LANES;
     const int64_t col = c0 + wc * 16 * CB + lane % LANES * N_CHUNK;
-    int64_t share = blockIdx.z * split.stride;   // where this share's sums begin
+    int64_t share = nth * split.stride;   // where this share's sums begin
     if constexpr (PRODUCT == kWeightGrad) {
         ep.out += (int64_t)expert * a.out_stride;
         share += (int64_t)expert * a.out_rows * ep.cols;
@@ -677,6 +677,12 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a,
     });
 }
 
+template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT>
+__global__ __launch_bounds__(256) void product_tile_kernel(const Operands<T_> a, const Epilogue<T_> ep, const TileOrder order, const Split split)
+{
+    product_tile<T_, PRODUCT, RB, CB, SHORT>(a, ep, order, split, blockIdx.x, blockIdx.y, blockIdx.z);
+}
+
 // The outputs of a product whose k was split: the shares' sums are added in their order and finished.  A thread owns 16
 // bytes of a row of the output, a workgroup 256 of them in 256 / lanes rows of one expert.
 template <typename T_, Product PRODUCT>
@@ -736,28 +742,27 @@ __global__ __launch_bounds__(256) void join_kernel(const Operands<T_> a, const E
 
 // ------------------------------------------------------------------ host side --
 // More LDS than a launch gets without asking: asked for once a kernel and device (0.9 us of a call otherwise).
-template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT>
-static hipError_t reserve_lds()
+template <auto KERNEL, int BYTES>
+static dass_status reserve_lds(const char *fn)
 {
     static std::atomic<uint64_t> done{0};
     int device = 0;
     hipError_t e = hipGetDevice(&device);
-    if (e != hipSuccess)
-        return e;
-    const uint64_t bit = device < 64 ? 1ull << device : 0;
-    if (done.load(std::memory_order_relaxed) & bit)
-        return hipSuccess;
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(product_tile_kernel<T_, PRODUCT, RB, CB, SHORT>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<SHORT>());
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (e == hipSuccess && (done.load(std::memory_order_relaxed) & bit))
+        return DASS_OK;
     if (e == hipSuccess)
-        done.fetch_or(bit, std::memory_order_relaxed);
-    return e;
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, BYTES);
+    if (e != hipSuccess)
+        return fail(DASS_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", fn, BYTES, hipGetErrorString(e));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return DASS_OK;
 }
 
-template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT = false>
-static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, const Split &split, hipStream_t stream)
+// The order of a product's tiles (for dW of one expert's); blocks: 0 if they are too many for a launch.
+template <typename T_, Product PRODUCT, int BR, int BC>
+static TileOrder order_tiles(const Operands<T_> &a, const Epilogue<T_> &ep)
 {
-    constexpr int BR = 32 * RB, BC = 32 * CB;
     const int64_t tiles_r = PRODUCT == kWeightGrad ? (a.out_rows + BR - 1) / BR : tile_numbers(a.seg, BR);
     const int64_t tiles_c = (ep.cols + BC - 1) / BC;
     const int64_t q_bytes = (PRODUCT == kWeightGrad ? a.seg.rows : a.depth) * ep.cols * (int64_t)sizeof(T_);
@@ -767,15 +772,22 @@ static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epi
         order.blocks = n <= 0x7fffffffLL ? (unsigned)n : 0;
         order.tiles_n = (unsigned)tiles_c;
     }
+    return order;
+}
+
+template <typename T_, Product PRODUCT, int RB, int CB, bool SHORT = false>
+static dass_status launch_tiles(const char *fn, const Operands<T_> &a, const Epilogue<T_> &ep, const Split &split, hipStream_t stream)
+{
+    const TileOrder order = order_tiles<T_, PRODUCT, 32 * RB, 32 * CB>(a, ep);
     const unsigned experts = PRODUCT == kWeightGrad ? a.seg.n : 1;
     if (order.blocks == 0 || (int64_t)order.blocks * 256 > 0xffffffffLL / experts / split.n)
         return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
-    const hipError_t e = reserve_lds<T_, PRODUCT, RB, CB, SHORT>();
-    if (e != hipSuccess)
-        return fail(DASS_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", fn, lds_bytes<SHORT>(), hipGetErrorString(e));
+    dass_status s = reserve_lds<product_tile_kernel<T_, PRODUCT, RB, CB, SHORT>, lds_bytes<SHORT>()>(fn);
+    if (s != DASS_OK)
+        return s;
     hipLaunchKernelGGL((product_tile_kernel<T_, PRODUCT, RB, CB, SHORT>), dim3(order.blocks, experts, split.n), dim3(256),
                        lds_bytes<SHORT>(), stream, a, ep, order, split);
-    dass_status s = check_launch("product kernel");
+    s = check_launch("product kernel");
     if (s != DASS_OK || split.n == 1)
         return s;
     constexpr int N = Chunk<T_>::N;

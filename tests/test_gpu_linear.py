@@ -272,6 +272,15 @@ def test_linear_backward_by_expert(gpu_device, T, E, tail, dtype):
     assert torch.all(got["dW"][empty] == 0) and torch.all(got["dbias"][empty] == 0)
 
 
+@pytest.mark.parametrize("dtype,T,d_in,d_out,E", LARGE[:19] + [("bf16", *size, 0) for size in SIZES])
+def test_linear_backward_one_by_one(gpu_device, dtype, T, d_in, d_out, E):
+    """Each product in a call of its own: both together may share a launch."""
+    p = _make(T, d_in, d_out, dtype, E=E, tail=31 if E else 0)
+    pre, dout = _saved(p, dtype)
+    for names in (("dX",), ("dW", "dbias")):
+        _check_backward(p, "silu", pre, dout, _backward(p, "silu", pre, dtype, names=names, dout=dout), dtype, f"{T} x {d_in} -> {d_out}")
+
+
 @pytest.mark.parametrize("names", [("dX",), ("dW",), ("dbias",), ("dmul",), ("dX", "dbias"), ("dW", "dmul")])
 def test_linear_backward_parts(gpu_device, names):
     """Each gradient alone has the bits that it has among the others."""
