@@ -269,8 +269,8 @@ struct FewGrads {
 };
 dass_status launch_few_grads(const char *fn, const FewGrads &grads, hipStream_t stream);
 
-// The same for both products with 128 x 128 tiles, none of them split (bf16); the bias sums where dbias is given.
-dass_status launch_pair(const char *fn, bool short_tiles, const Operands<uint16_t> &ax, const Epilogue<uint16_t> &ex,
-                        const Operands<uint16_t> &aw, const Epilogue<uint16_t> &ew, const BiasSums &bias, hipStream_t stream);
+// The same for both products with the same tiles (Plan), none of them split (bf16); the bias sums where dbias is given.
+dass_status launch_pair(const char *fn, int tile, const Operands<uint16_t> &ax, const Epilogue<uint16_t> &ex, const Operands<uint16_t> &aw,
+                        const Epilogue<uint16_t> &ew, const BiasSums &bias, hipStream_t stream);
 
 }  // namespace dass

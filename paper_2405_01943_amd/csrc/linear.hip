@@ -298,25 +298,46 @@ static Plan plan_of(Product product, int dt, int64_t T, int64_t d_in, int64_t d_
     return plan_product(product, dt, n_experts, d_out, d_in, (T + n_experts - 1) / n_experts);
 }
 
-// Whether both products of a bf16 gradient (and its bias sums) go into one launch, with 128 x 128 tiles (2), short ones (3) or not
-// at all (0): beside each other the tiles of two small products take as long as the longer one, or beyond one round their work
-// over the slots and half a tile.  In graphs, with the element-wise pass and bias sums: 301 rows of 256 x 688 22.0 us, in one launch
-// 13.1; 1030 of 576 x 520 29.4, 18.2; 1024 of 2048 x 2048 44.1, 32.7; 2000 rows over 8 experts of 512 x 1024 35.3, 22.9;
-// but 512 of 1024 x 4096 34.0, 43.1, where each alone fills the chip, and 16384 of 512 x 512 57.5, 170.8, where k has to be split.  Over 50
-// sizes the choice is 1 % slower than the best in the mean, and 1.29 times as fast as two launches always.
+// When n1 workgroups of t1 and after them n2 of t2 <= t1 are done on `slots` places, each taking the next one when it is free.
+static double makespan(int64_t n1, double t1, int64_t n2, double t2, int64_t slots)
+{
+    const int64_t rounds = n1 / slots, late = n1 % slots;   // late: places that have one more of the first
+    const double from[2] = {rounds * t1, (rounds + 1) * t1};
+    const auto done = [&](double t) {   // of the second, at time t
+        const auto each = [&](double begin) { return t < begin ? 0 : (int64_t)((t - begin) / t2 + 1e-6); };
+        return late * each(from[1]) + (slots - late) * each(from[0]);
+    };
+    double first = 1e300;
+    for (int i = 0; i < (late ? 2 : 1); ++i) {
+        int64_t m = std::max((int64_t)0, n2 / slots - (i ? (int64_t)(t1 / t2) + 1 : 0));
+        while (done(from[i] + m * t2) < n2)
+            ++m;
+        first = std::min(first, from[i] + m * t2);
+    }
+    return std::max(first, late ? from[1] : from[0]);
+}
+
+// The tile of both products of a bf16 gradient (and its bias sums) in one launch, or -1 for a launch each: the tiles of the one
+// fill the rounds that the other leaves, the longer ones first.  In graphs, with the element-wise pass and bias sums: 301 rows of
+// 256 x 688 22.0 us, in one launch 13.1; 1030 of 576 x 520 29.4, 18.2; 2000 rows over 8 experts of 512 x 1024 35.3, 22.9; 4100 of 2056 x
+// 2056 159, 113 with 256 x 256; 8192 over 8 experts of 4096 x 14336 2000, 1863; but 512 of 1024 x 4096 34.0, 43.1, and 16384
+// of 512 x 512 57.5, 170.8, where k has to be split.  Over 97 sizes the choice is 1 % slower than the best in the mean, and 1.26
+// times as fast as two launches always.
 static int pair_of(const Plan &x, const Plan &w, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
 {
-    const int64_t tiles_x = row_tiles(kInputGrad, n_experts, T, 128) * pieces(d_in, 128);
-    const int64_t tiles_w = n_experts * pieces(d_out, 128) * pieces(d_in, 128), tiles = tiles_x + tiles_w;
-    if (tiles > 1 << 20)
-        return 0;
     const int64_t slabs_x = pieces(d_out, 64), slabs_w = pieces(pieces(T, n_experts), 64);
     const double memory = 6 + 2.0 / 5.2e6 * std::min(n_experts, T) * d_in * d_out + 2.0 / 3.38e6 * ((double)T + n_experts * d_out) * d_in;
-    int best = 0;
+    int best = -1;
     double best_time = x.us + w.us + 2;   // 2: the second launch
-    for (int k = 2; k <= 3; ++k) {
-        const double one_x = kTiles[k].time(slabs_x, tiles), one_w = kTiles[k].time(slabs_w, tiles), longer = std::max(one_x, one_w);
-        const double busy = tiles <= kTiles[k].slots ? longer : (tiles_x * one_x + tiles_w * one_w) / kTiles[k].slots + longer / 2;
+    for (int k = 0; k <= 3; ++k) {
+        const Tile &t = kTiles[k];
+        const int64_t tiles_x = row_tiles(kInputGrad, n_experts, T, t.rows) * pieces(d_in, t.cols);
+        const int64_t tiles_w = n_experts * pieces(d_out, t.rows) * pieces(d_in, t.cols), tiles = tiles_x + tiles_w;
+        const double one_x = t.time(slabs_x, tiles), one_w = t.time(slabs_w, tiles);
+        if (tiles > 1 << 20 || (tiles_x * one_x + tiles_w * one_w) / t.slots >= best_time)
+            continue;
+        const double busy = slabs_x >= slabs_w ? makespan(tiles_x, one_x, tiles_w, one_w, t.slots)
+                                               : makespan(tiles_w, one_w, tiles_x, one_x, t.slots);
         const double time = std::max(busy, memory);
         if (time < best_time) {
             best_time = time;
@@ -339,7 +360,7 @@ static size_t split_bytes(const Plan &plan, Product product, int64_t T, int64_t 
 // What a gradient's call takes and needs: g if it is kept, then the most of the bias sums and of the split products' shares.
 struct GradPlan {
     Plan x, w;
-    int pair;
+    int pair;   // the tile of both products in one launch; -1: none
     size_t bytes;
 };
 
@@ -347,6 +368,7 @@ static GradPlan plan_grad(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt,
                           bool dbias)
 {
     GradPlan p = {};
+    p.pair = -1;
     if (dX)
         p.x = plan_of(kInputGrad, dt, T, d_in, d_out, n_experts);
     if (dW)
@@ -354,9 +376,9 @@ static GradPlan plan_grad(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt,
     if (dX && dW && dt == DASS_BF16)
         p.pair = pair_of(p.x, p.w, T, d_in, d_out, n_experts);
     p.bytes = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
-    if (dX && !p.pair)
+    if (dX && p.pair < 0)
         p.bytes = std::max(p.bytes, split_bytes(p.x, kInputGrad, T, d_in, d_out, n_experts));
-    if (dW && !p.pair)
+    if (dW && p.pair < 0)
         p.bytes = std::max(p.bytes, split_bytes(p.w, kWeightGrad, T, d_in, d_out, n_experts));
     p.bytes += keeps_g ? kept_bytes(T, d_out, dt) : 0;
     return p;
@@ -446,8 +468,8 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     // with the few tiles of the products, if no split product takes the partial sums' place
     const bool bias_with_few = (few_x || few_w) && !tiles_x && !tiles_w && (t.d_out + 63) / 64 * t.n_experts <= 1 << 20;
     if constexpr (sizeof(T_) == 2) {
-        if (plan.pair)
-            return launch_pair(fn, plan.pair == 3, ax, ex, aw, ew, bias, stream);
+        if (plan.pair >= 0)
+            return launch_pair(fn, plan.pair, ax, ex, aw, ew, bias, stream);
     }
     if (t.dbias && !bias_with_few) {
         hipLaunchKernelGGL(bias_kernel<T_>, dim3((unsigned)((t.d_out + 63) / 64), (unsigned)t.n_experts), dim3(256), 0, stream, bias);
