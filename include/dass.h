@@ -435,7 +435,7 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  * they were in dX and dmul.  pre may be NULL if act is DASS_ACT_NONE and
  * dmul is not asked for.  Outputs must not overlap inputs.  g is rounded to dt for the two products, and dbias
  * is summed before that; everything else is f32 and rounded once.  Sums have a fixed order: the same
- * bits on every run.
+ * call gives the same bits on every run (with other gradients asked for, k may be split otherwise).
  *   workspace  dass_linear_backward_workspace_bytes() bytes, 16-byte aligned: g
  *            and partial sums.  A call without activation and mul, or of fewer
  *            gradients, needs less and takes less.

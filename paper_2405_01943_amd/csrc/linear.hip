@@ -132,7 +132,7 @@ static size_t partial_bytes(int64_t rows, int64_t d_out, int64_t n_experts, int 
 // The longest row stride of an operand of the products, in elements: 256 of them stay below 2^31 bytes.
 static int64_t longest_read(int dt) { return kMaxReadRow / (dt == DASS_BF16 ? 2 : 4) - vec_elems(dt); }
 
-struct Checker {
+struct Arguments {
     const char *fn;
     int vec;
     dass_status status = DASS_OK;
@@ -513,7 +513,7 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
     if (!task)
         return fail(DASS_ERR_NULL, "%s: task must not be NULL", fn);
     const dass_linear_task &t = *task;
-    Checker c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
+    Arguments c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
     c.sizes(t.T, t.d_in, t.d_out, t.n_experts, t.offsets, (int)t.dt, (int)t.act);
     const int64_t read = longest_read(t.dt);
     c.matrix("X", t.X, t.ldx, t.d_in, true, read);
@@ -560,7 +560,7 @@ extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, v
     if (!task)
         return fail(DASS_ERR_NULL, "%s: task must not be NULL", fn);
     const dass_linear_grad_task &t = *task;
-    Checker c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
+    Arguments c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
     c.sizes(t.T, t.d_in, t.d_out, t.n_experts, t.offsets, (int)t.dt, (int)t.act);
     if (c.status != DASS_OK)
         return c.status;

@@ -99,6 +99,17 @@ def test_strange_offsets_stay_inside(gpu_device, bounds):
             _run(part, pre[:T], dout[:T], 3)
 
 
+@pytest.mark.parametrize("names", [("dX",), ("dW",), ("dbias",), ("dX", "dbias"), ("dW", "dmul"), ("dX", "dW"), ("dW", "dbias")])
+@pytest.mark.parametrize("E", [0, 3])
+def test_small_f32_gradients_in_any_company(gpu_device, E, names):
+    """The parts of the one launch of a small f32 gradient: each alone and with others has the same bits."""
+    p = _make(90, 136, 72, "f32", E=E, tail=4 if E else 0)
+    pre, dout = _saved(p, "f32")
+    whole, part = (_backward(p, "silu", pre, "f32", names=n, dout=dout) for n in (("dX", "dW", "dbias", "dmul"), names))
+    for name in names:
+        assert torch.equal(part[name].view(torch.int32), whole[name].view(torch.int32)), name
+
+
 # ------------------------------------------------------- beyond 2^31 elements --
 FAR = 300      # the last rows, all that is compared
 
