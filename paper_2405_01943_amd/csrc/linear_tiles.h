@@ -71,11 +71,13 @@ constexpr int lds_bytes()
 }
 constexpr int kOutside = 0x7fffffff;
 
-// A raw buffer: 48 bits of address, no stride, its length in bytes.
+// A raw buffer: 48 bits of address, no stride, its length in bytes.  Its words, the same in every lane, are put into scalar registers
+// here, as the loads by hand need them; left to itself the compiler does so with every optimisation on alone.
 __device__ __forceinline__ u32x4 raw_buffer(const void *p, int bytes)
 {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
-    return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+    const auto scalar = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+    return u32x4{scalar((uint32_t)a), scalar((uint32_t)(a >> 32) & 0xffffu), scalar((uint32_t)bytes), 0x00020000u};
 }
 
 // One wave-load of 16 bytes a lane from a buffer straight into LDS: the builtin where both operands are by rows, and
