@@ -44,8 +44,8 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E
 # size (FETCH_SIZE x 2.0, WRITE_SIZE x 1.0; see profiles/).  A figure only stands while the source
 # of its kernel is the one the counters were taken on; otherwise `traffic` is null.
 MEASURED_TRAFFIC = {
-    "stage1": {"sources": ("calib.hip", "tile_order.h"),
-               "sha256": "84931e6a59fa4bffb1b2cd62e398d8640fe910f7e3b001f4de554d0b4daf2489",
+    "stage1": {"sources": ("calib.hip", "activations.h", "tile_order.h"),
+               "sha256": "5ea7f41e47fd93ee6e49ff3552d7de4503fcfd3653fecb98576ef7f16fea7400",
                "bytes": (38209297 * 2.0 + 88064) * 1024},
     # the step's two batched launches: Gate + Up, Down
     "stage2": {"sources": ("nm.hip", "select.h"), "sha256": "6e0c1d7b4feaa3f4533cbef910c1dec8f06fc37d7cf336a813278e5259bdbcc9",
