@@ -189,6 +189,7 @@ struct Operands {
     int64_t out_stride;    // dW: elements from one expert's C to the next
     int64_t out_rows;      // dW: rows of C
     int64_t depth;         // forward, dX: k
+    int64_t lo;            // > 0: P is g in two parts, the second `lo` elements behind the first, and k runs over both
     Segments seg;
 };
 

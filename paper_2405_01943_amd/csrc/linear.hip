@@ -5,7 +5,9 @@
 // Gradients, with g = dout * mul * act'(pre):  dX = g W,  dW = g^T X over an expert's rows,  db = sum of its g,
 // dmul = dout * act(pre).  g is read by both products, so it is written once, in dtype dt: rounded to bf16
 // there because the matrix cores take nothing wider (each term of a sum is off by half a step of its own, which adds about as
-// much to a sum as its own rounding does).  Without activation and mul, g is dout itself and nothing is written.
+// much to a sum as its own rounding does: 0.0023 of the whole where f32 would leave 0.0017).  Where g or dX is small
+// chance makes it more (two rows of 144: 0.0026), and there g is kept as two bf16 numbers, the rounded one and what that left,
+// and the products run over both.  Without activation and mul, g is dout itself and nothing is written.
 #include "linear.h"
 
 #include <algorithm>
@@ -23,8 +25,8 @@ constexpr int64_t kMaxReadRow = 1 << 23;   // bytes between rows that a tile add
 template <typename T_>
 __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout, int64_t ldg, const T_ *__restrict__ pre,
                                                     int64_t ldp, const T_ *__restrict__ mul, int64_t ldm, int act, int64_t cols,
-                                                    Segments seg, int tile_rows, T_ *__restrict__ g_out, T_ *__restrict__ dmul,
-                                                    int64_t lddm, float *__restrict__ partial, uint32_t strips)
+                                                    Segments seg, int tile_rows, T_ *__restrict__ g_out, int64_t ldk, int64_t lo,
+                                                    T_ *__restrict__ dmul, int64_t lddm, float *__restrict__ partial, uint32_t strips)
 {
     constexpr int N = Chunk<T_>::N;
     constexpr bool FAST = sizeof(T_) == 2;
@@ -72,12 +74,25 @@ __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout,
                 for (int x = 0; x < N; ++x)
                     g[x] *= y[x];
             }
-            if (g_out)
-                *reinterpret_cast<u32x4 *>(g_out + row * cols + c) = Chunk<T_>::narrow(g);
 #pragma unroll
             for (int x = 0; x < N; ++x)
                 sum[x] += g[x];
+            if (g_out) {
+                const u32x4 rounded = Chunk<T_>::narrow(g);
+                *reinterpret_cast<u32x4 *>(g_out + row * ldk + c) = rounded;
+                if (lo > 0) {
+                    float h[N];
+                    Chunk<T_>::widen(rounded, h);
+#pragma unroll
+                    for (int x = 0; x < N; ++x)
+                        g[x] = fabsf(h[x]) < INFINITY ? g[x] - h[x] : 0.0f;
+                    *reinterpret_cast<u32x4 *>(g_out + row * ldk + lo + c) = Chunk<T_>::narrow(g);
+                }
+            }
         }
+    } else if (g_out && c < lo) {   // to whole slabs
+        for (int64_t row = r.lo + wave; row < end; row += 4)
+            *reinterpret_cast<u32x4 *>(g_out + row * ldk + c) = *reinterpret_cast<u32x4 *>(g_out + row * ldk + lo + c) = u32x4{0, 0, 0, 0};
     }
     if (!partial)
         return;
@@ -119,9 +134,24 @@ static int sum_tile_rows(int64_t rows, int64_t cols, int dt)
     return (int)(t < (1 << 24) ? t : 1 << 24);
 }
 
-static size_t kept_bytes(int64_t rows, int64_t d_out, dass_dtype dt)
+// Elements from a row's g to the second part of it, whole slabs; 0: g is in one part.  In two where it has up to 16384 elements, or dX
+// up to 8192: of more the mean squares of the errors are within a quarter of their expectation (30000 gradients of random
+// sizes: off by at most 1.5 times what the result's rounding alone is, in one part up to 1.63 times with two rows of dX).
+static int64_t second_part(int64_t rows, int64_t d_in, int64_t d_out, int dt)
 {
-    return round_up((size_t)rows * (size_t)d_out * elem_bytes(dt), 256);
+    return dt == DASS_BF16 && (rows * d_out <= 16384 || rows * d_in <= 8192) ? round_up((size_t)d_out, 64) : 0;
+}
+
+// Elements of a row of the g that is kept.
+static int64_t kept_row(int64_t rows, int64_t d_in, int64_t d_out, int dt)
+{
+    const int64_t lo = second_part(rows, d_in, d_out, dt);
+    return lo > 0 ? 2 * lo : d_out;
+}
+
+static size_t kept_bytes(int64_t rows, int64_t d_in, int64_t d_out, dass_dtype dt)
+{
+    return round_up((size_t)rows * (size_t)kept_row(rows, d_in, d_out, dt) * elem_bytes(dt), 256);
 }
 
 static size_t partial_bytes(int64_t rows, int64_t d_out, int64_t n_experts, int dt)
@@ -238,14 +268,14 @@ static const Tile kTiles[] = {{256, 256, 256, 8.8, 1.34}, {128, 256, 256, 5.4, 0
 //           (bf16, forward only) the weights' bytes, or one workgroup's.  Up to 8 rows: one row of 2048 x 32000 30.0 us (tiles
 //           36.5), 8 of it 34.5 (37.7); but one row of 16384 x 1024 20.6 (tiles with 16 shares 15.6).  16 rows over 8 experts
 //           of 4096 x 14336 171 (186), 64 over 8 204 (182).
-static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, int64_t cols, int64_t depth)
+static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, int64_t cols, int64_t depth, int parts = 1)
 {
     const bool bf16 = dt == DASS_BF16;
     const int64_t share = product == kWeightGrad ? rows : pieces(rows, groups);   // of an expert, were they even
     const int64_t used = std::min(groups, rows);
     static const int kShares[] = {1, 2, 3, 4, 6, 8, 12, 16};
     const double join = bf16 ? 3.64 : 2.4, byte = bf16 ? 1 / 6.13e6 : 1 / 4.5e6;   // us, us a byte
-    const int64_t slabs = pieces(depth, bf16 ? 64 : 32), outputs = (product == kWeightGrad ? groups : 1) * rows * cols;
+    const int64_t slabs = parts * pieces(depth, bf16 ? 64 : 32), outputs = (product == kWeightGrad ? groups : 1) * rows * cols;
     const double weights = product == kWeightGrad ? 0 : (bf16 ? 6 : 0) + (bf16 ? 2.0 / 5.2e6 : 4.0 / 4.6e6) * used * cols * depth;
     const double written = bf16 ? 2.0 / 3.38e6 * outputs : 0;
     Plan best = {Plan::kTiles, bf16 ? 0 : 2, 1, 0, 0};
@@ -289,13 +319,14 @@ static Plan plan_product(Product product, int dt, int64_t groups, int64_t rows, 
     return best;
 }
 
-static Plan plan_of(Product product, int dt, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+// parts: of g, that k runs over
+static Plan plan_of(Product product, int dt, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts, int parts = 1)
 {
     if (product == kForward)
         return plan_product(product, dt, n_experts, T, d_out, d_in);
     if (product == kInputGrad)
-        return plan_product(product, dt, n_experts, T, d_in, d_out);
-    return plan_product(product, dt, n_experts, d_out, d_in, (T + n_experts - 1) / n_experts);
+        return plan_product(product, dt, n_experts, T, d_in, d_out, parts);
+    return plan_product(product, dt, n_experts, d_out, d_in, (T + n_experts - 1) / n_experts, parts);
 }
 
 // When n1 workgroups of t1 and after them n2 of t2 <= t1 are done on `slots` places, each taking the next one when it is free.
@@ -323,9 +354,9 @@ static double makespan(int64_t n1, double t1, int64_t n2, double t2, int64_t slo
 // 2056 159, 113 with 256 x 256; 8192 over 8 experts of 4096 x 14336 2000, 1863; but 512 of 1024 x 4096 34.0, 43.1, and 16384
 // of 512 x 512 57.5, 170.8, where k has to be split.  Over 97 sizes the choice is 1 % slower than the best in the mean, and 1.26
 // times as fast as two launches always.
-static int pair_of(const Plan &x, const Plan &w, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts)
+static int pair_of(const Plan &x, const Plan &w, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts, int parts)
 {
-    const int64_t slabs_x = pieces(d_out, 64), slabs_w = pieces(pieces(T, n_experts), 64);
+    const int64_t slabs_x = parts * pieces(d_out, 64), slabs_w = parts * pieces(pieces(T, n_experts), 64);
     const double memory = 6 + 2.0 / 5.2e6 * std::min(n_experts, T) * d_in * d_out + 2.0 / 3.38e6 * ((double)T + n_experts * d_out) * d_in;
     int best = -1;
     double best_time = x.us + w.us + 2;   // 2: the second launch
@@ -367,20 +398,21 @@ struct GradPlan {
 static GradPlan plan_grad(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW,
                           bool dbias)
 {
+    const int parts = keeps_g && second_part(T, d_in, d_out, dt) > 0 ? 2 : 1;
     GradPlan p = {};
     p.pair = -1;
     if (dX)
-        p.x = plan_of(kInputGrad, dt, T, d_in, d_out, n_experts);
+        p.x = plan_of(kInputGrad, dt, T, d_in, d_out, n_experts, parts);
     if (dW)
-        p.w = plan_of(kWeightGrad, dt, T, d_in, d_out, n_experts);
+        p.w = plan_of(kWeightGrad, dt, T, d_in, d_out, n_experts, parts);
     if (dX && dW && dt == DASS_BF16)
-        p.pair = pair_of(p.x, p.w, T, d_in, d_out, n_experts);
+        p.pair = pair_of(p.x, p.w, T, d_in, d_out, n_experts, parts);
     p.bytes = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
     if (dX && p.pair < 0)
         p.bytes = std::max(p.bytes, split_bytes(p.x, kInputGrad, T, d_in, d_out, n_experts));
     if (dW && p.pair < 0)
         p.bytes = std::max(p.bytes, split_bytes(p.w, kWeightGrad, T, d_in, d_out, n_experts));
-    p.bytes += keeps_g ? kept_bytes(T, d_out, dt) : 0;
+    p.bytes += keeps_g ? kept_bytes(T, d_in, d_out, dt) : 0;
     return p;
 }
 
@@ -421,10 +453,11 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     constexpr int N = Chunk<T_>::N;
     const Segments seg = {t.offsets, t.T, (int)t.n_experts};
     const bool own_g = keeps_g(t);
+    const int64_t lo = own_g ? second_part(t.T, t.d_in, t.d_out, t.dt) : 0, ldk = kept_row(t.T, t.d_in, t.d_out, t.dt);
     const T_ *g = static_cast<const T_ *>(t.dout);
     int64_t ldg = t.ldg;
     // the workspace: g if it is kept, then the partial sums of the bias, whose place the split products take after them
-    char *const shares = workspace + (own_g ? kept_bytes(t.T, t.d_out, t.dt) : 0);
+    char *const shares = workspace + (own_g ? kept_bytes(t.T, t.d_in, t.d_out, t.dt) : 0);
     const BiasSums bias = {reinterpret_cast<float *>(shares), t.d_out, seg, sum_tile_rows(t.T, t.d_out, t.dt), t.dbias};
     if (own_g || t.dbias || t.dmul) {
         T_ *kept = own_g ? reinterpret_cast<T_ *>(workspace) : nullptr;
@@ -433,14 +466,14 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
             return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
         hipLaunchKernelGGL(slope_kernel<T_>, dim3((unsigned)(numbers * strips)), dim3(256), 0, stream,
                            static_cast<const T_ *>(t.dout), t.ldg, static_cast<const T_ *>(t.pre), t.ldp,
-                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, bias.tile_rows, kept,
+                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, bias.tile_rows, kept, ldk, lo,
                            static_cast<T_ *>(t.dmul), t.lddm, t.dbias ? reinterpret_cast<float *>(shares) : nullptr, (uint32_t)strips);
         const dass_status s = check_launch("slope kernel");
         if (s != DASS_OK)
             return s;
         if (own_g) {
             g = kept;
-            ldg = t.d_out;
+            ldg = ldk;
         }
     }
 
@@ -448,6 +481,7 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     Epilogue<T_> ex = {}, ew = {};
     ax.P = aw.P = g;
     ax.ldp = aw.ldp = ldg;
+    ax.lo = aw.lo = lo;
     ax.seg = aw.seg = seg;
     ex.cols = ew.cols = t.d_in;
     ex.act = ew.act = DASS_ACT_NONE;
@@ -546,10 +580,13 @@ extern "C" size_t dass_linear_backward_workspace_bytes(int64_t T, int64_t d_in, 
     if (T <= 0 || d_in <= 0 || d_out <= 0 || n_experts <= 0 || n_experts > kMaxLinearExperts || !valid_dtype(dt) || T > kMaxRows ||
         d_in > kMaxWidth || d_out > kMaxWidth)
         return 0;
-    // the most that a call of all or some of the gradients needs: one alone may be split where both together are not
-    return std::max(plan_grad(T, d_in, d_out, dt, n_experts, true, true, false, true).bytes,
-                    std::max(plan_grad(T, d_in, d_out, dt, n_experts, true, false, true, true).bytes,
-                             plan_grad(T, d_in, d_out, dt, n_experts, true, true, true, true).bytes));
+    // the most that a call of all or some of the gradients needs: one alone may be split where both together are not, and a g
+    // that is not kept may be split otherwise
+    size_t most = 0;
+    for (const bool keeps : {false, true})
+        for (const int which : {1, 2, 3})
+            most = std::max(most, plan_grad(T, d_in, d_out, dt, n_experts, keeps, which & 1, which & 2, true).bytes);
+    return most;
 }
 
 extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, void *workspace, size_t workspace_bytes,

@@ -169,10 +169,18 @@ struct Lines {
     static constexpr int LINE = 32 * B * E, SLOTS = LINE / 16, LINES = 1024 / LINE;   // bytes, chunks; lines of a wave-load
     static_assert(LINES * LINE == 1024 && LINES > 0, "whole lines");
     const T_ *m;
-    int64_t ld, depth, width;
+    int64_t ld, depth, width, lo = 0;
+    int first = 0, fold = 0x7fffffff;
     u32x4 buffer;
     uint32_t off[LOADS];
 
+    // k runs over the same `slabs` slabs twice, this workgroup's beginning with the `begin`-th; the second time `lo_` elements further on.
+    __device__ __forceinline__ void twice(int begin, int slabs, int64_t lo_)
+    {
+        first = begin;
+        fold = slabs;
+        lo = lo_;
+    }
     // swap(line): what the place of a 16-byte chunk is XORed with
     template <typename F>
     __device__ __forceinline__ void init_lines(const T_ *base, int64_t ld_, int64_t row0, int64_t rows, int64_t k0, int64_t k, int wave, int lane, F swap)
@@ -189,8 +197,16 @@ struct Lines {
     }
     __device__ __forceinline__ void begin_slab(int slab)
     {
+        const T_ *from = m;
+        if constexpr (BY_HAND) {
+            slab += first;
+            if (slab >= fold) {
+                slab -= fold;
+                from += lo;
+            }
+        }
         const int64_t left = depth - (int64_t)slab * SLAB, lines = left < SLAB ? left : SLAB;
-        buffer = raw_buffer(m + (int64_t)slab * SLAB * ld, (int)(((lines - 1) * ld + width) * E));
+        buffer = raw_buffer(from + (int64_t)slab * SLAB * ld, (int)(((lines - 1) * ld + width) * E));
     }
     template <bool LAST>
     __device__ __forceinline__ void load(char *unit, int wave, int, int q) const
@@ -377,17 +393,32 @@ __device__ __forceinline__ void product_tile(const Operands<T_> &a, const Epilog
         for (int j = 0; j < RB; ++j)
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+    const int64_t once = depth;
+    const bool two = BY_HAND && a.lo > 0;   // g in two parts: k runs over them one after the other, whole slabs of each
+    const int fold = (int)((once + SLAB - 1) / SLAB);
+    if (two)
+        depth = 2 * (int64_t)fold * SLAB;
+    int64_t from = 0;
     if (split.n > 1) {   // this workgroup's share of the slabs, perhaps none
-        const int64_t share = ((depth + SLAB - 1) / SLAB + split.n - 1) / split.n * SLAB, from = share * nth;
+        const int64_t share = ((depth + SLAB - 1) / SLAB + split.n - 1) / split.n * SLAB;
+        from = share * nth;
         depth = from >= depth ? 0 : depth - from < share ? depth - from : share;
-        k0 += from;
     }
     const int S = (int)((depth + SLAB - 1) / SLAB);
     if (S > 0) {
     PartP P;
     PartQ Q;
-    P.init(a.P, a.ldp, r0, r_end, k0, depth, wave, lane, wr);
-    Q.init(PRODUCT == kWeightGrad ? a.Q : a.Q + (int64_t)expert * a.q_stride, a.ldq, c0, ep0.cols, k0, depth, wave, lane, wc);
+    const T_ *const q = PRODUCT == kWeightGrad ? a.Q : a.Q + (int64_t)expert * a.q_stride;
+    const bool p_folds = two && PRODUCT == kWeightGrad;   // (by rows the parts are one row)
+    P.init(a.P, a.ldp, r0, r_end, p_folds ? k0 : k0 + from, p_folds ? once : depth, wave, lane, wr);
+    Q.init(q, a.ldq, c0, ep0.cols, two ? k0 : k0 + from, two ? once : depth, wave, lane, wc);
+    if constexpr (BY_HAND) {
+        if (two) {
+            if constexpr (PRODUCT == kWeightGrad)
+                P.twice((int)(from / SLAB), fold, a.lo);
+            Q.twice((int)(from / SLAB), fold, 0);
+        }
+    }
     char *const p_ring = lds, *const q_ring = lds + NP * PartP::UNIT;
 
     // ---- the loads.  Iteration t (after the barrier of slab t) requests the follower's slab t + NF, then the leader's t + ND.

@@ -8,7 +8,7 @@ import paper_2405_01943_amd as dass
 from paper_2405_01943_amd import binding
 
 import linear_reference as ref
-from test_gpu_linear import DT, _backward, _check_backward, _check_forward, _forward, _make, _saved, _u
+from test_gpu_linear import DT, V, _backward, _check_backward, _check_forward, _forward, _make, _saved, _u, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -108,6 +108,24 @@ def test_small_f32_gradients_in_any_company(gpu_device, E, names):
     whole, part = (_backward(p, "silu", pre, "f32", names=n, dout=dout) for n in (("dX", "dW", "dbias", "dmul"), names))
     for name in names:
         assert torch.equal(part[name].view(torch.int32), whole[name].view(torch.int32)), name
+
+
+@pytest.mark.parametrize("names", [("dX", "dW"), ("dX",), ("dW",)])
+@pytest.mark.parametrize("T,d_in,d_out,E", [(1, 128, 128, 0), (1, 4096, 264, 0), (2, 128, 8192, 0), (4, 1000, 4096, 0), (40, 136, 200, 3),
+                                            (150, 64, 104, 0), (2048, 72, 8, 0), (250, 1032, 64, 9), (1, 2056, 14336, 5), (65, 64, 72, 0), (3, 136, 14336, 0), (33, 200, 5000, 4)])
+def test_gradients_of_few_elements_keep_more_of_g(gpu_device, T, d_in, d_out, E, names):
+    """Up to 16384 elements of g, or of a g with up to 8192 of dX, are two bf16 numbers: rounded twice they are off by at most 2^-8 of 2^-8."""
+    p = _make(T, d_in, d_out, "bf16", E=E, tail=min(T - 1, 3) if E else 0)
+    pre, dout = _saved(p, "bf16")
+    got = _backward(p, "silu", pre, "bf16", names=names, dout=dout)
+    want = ref.linear_grad(dout, p["X"], p["W"], p["offsets"], "silu", pre, p["mul"])
+    longest = max(hi - lo for _, lo, hi in ref.spans(T, p["offsets"]))
+    for name, K in (("dX", d_out), ("dW", longest)):
+        if name in got:
+            value, A, R = want[name]
+            # the result's rounding; g's two and 4 in f32; 4 sqrt(2 K) for the sum over both parts; the slope's own error
+            tol = _u(torch.bfloat16) * value.abs() + (2.0 ** -16 + 8 * V + 4 * math.sqrt(2 * K) * V) * A + 2.0 ** -20 * R
+            _within(got[name].reshape(value.shape), value, tol, f"{name} of {T} x {d_in} -> {d_out}, {E} experts")
 
 
 # ------------------------------------------------------- beyond 2^31 elements --
