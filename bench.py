@@ -45,7 +45,7 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E
 # of its kernel is the one the counters were taken on; otherwise `traffic` is null.
 MEASURED_TRAFFIC = {
     "stage1": {"sources": ("calib.hip", "activations.h", "tile_order.h"),
-               "sha256": "5ea7f41e47fd93ee6e49ff3552d7de4503fcfd3653fecb98576ef7f16fea7400",
+               "sha256": "7f865b83cce596222ec7d149b09414b31a8ff9e42d3aceaa2a4837a451bf97a8",
                "bytes": (38209297 * 2.0 + 88064) * 1024},
     # the step's two batched launches: Gate + Up, Down
     "stage2": {"sources": ("nm.hip", "select.h"), "sha256": "6e0c1d7b4feaa3f4533cbef910c1dec8f06fc37d7cf336a813278e5259bdbcc9",

@@ -54,7 +54,8 @@ __device__ __forceinline__ float glu_act_precise(float g, int act)
 }
 
 // The same with none among them, for the linear layers.  FAST: the hardware's exponential and reciprocal, for results
-// that are rounded to bf16.  The precise GELU takes erfc, which keeps its digits where 1 + erf cancels.
+// that are rounded to bf16.  The precise GELU takes erfc, which keeps its digits where 1 + erf cancels.  NaN stays NaN in every
+// value and slope: maxima and minima would drop it, so relu and the slope of gelu_tanh compare.
 template <bool FAST>
 __device__ __forceinline__ float act_value(float x, int act)
 {
@@ -68,7 +69,7 @@ __device__ __forceinline__ float act_value(float x, int act)
     case DASS_ACT_GELU_ERF:
         return FAST ? glu_act_fast<DASS_ACT_GELU_ERF>(x) : 0.5f * x * erfcf(-0.7071067811865476f * x);
     default:
-        return fmaxf(x, 0.0f);
+        return x <= 0.0f ? 0.0f : x;
     }
 }
 
@@ -106,7 +107,7 @@ __device__ __forceinline__ void act_values(float (&v)[N], int act)
 //   gelu_tanh  s + x s (1 - s) z',      s = 1 / (1 + exp(-z)), z = 2 sqrt(2/pi) (x + 0.044715 x^3); x is held to
 //              [-12, 12], where the slope is 0 and 1 to every bit, so that no overflow of z' meets a zero
 //   gelu_erf   Phi(x) + x exp(-x^2 / 2) / sqrt(2 pi)
-//   relu       1 for x > 0, else 0
+//   relu       1 for x > 0, 0 for x <= 0
 template <bool FAST>
 __device__ __forceinline__ float act_slope(float x, int act)
 {
@@ -119,7 +120,7 @@ __device__ __forceinline__ float act_slope(float x, int act)
         return s * fmaf(x, 1.0f - s, 1.0f);
     }
     case DASS_ACT_GELU_TANH: {
-        const float c = fminf(fmaxf(x, -12.0f), 12.0f), c2 = c * c;
+        const float c = x > 12.0f ? 12.0f : x < -12.0f ? -12.0f : x, c2 = c * c;
         const float z = 1.5957691216057308f * c * fmaf(0.044715f, c2, 1.0f);
         const float s = FAST ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z))
                              : 1.0f / (1.0f + expf(-z));
@@ -143,7 +144,7 @@ __device__ __forceinline__ float act_slope(float x, int act)
         return fmaf(0.3989422804014327f * x, bell, cdf);
     }
     default:
-        return x > 0.0f ? 1.0f : 0.0f;
+        return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
     }
 }
 
