@@ -6,7 +6,7 @@
 // dmul = dout * act(pre).  g is read by both products, so it is written once, in dtype dt: rounded to bf16
 // there because the matrix cores take nothing wider (each term of a sum is off by half a step of its own, which adds about as
 // much to a sum as its own rounding does: 0.0023 of the whole where f32 would leave 0.0017).  Where g or dX is small
-// chance makes it more (two rows of 144: 0.0026), and there g is kept as two bf16 numbers, the rounded one and what that left,
+// chance makes it more (two rows of 144: 0.0026), and there g is kept as two bf16 numbers, its leading bits and what they leave,
 // and the products run over both.  Without activation and mul, g is dout itself and nothing is written.
 #include "linear.h"
 
@@ -20,6 +20,19 @@ constexpr int64_t kMaxRows = 1 << 30, kMaxWidth = 1 << 20, kMaxStride = 1LL << 3
 constexpr int64_t kMaxReadRow = 1 << 23;   // bytes between rows that a tile addresses: 256 of them with 32-bit offsets
 
 // ------------------------------------------------------ element-wise gradient and sums --
+// g as two bf16 numbers: its leading bits, returned, and what they leave, to `rest` (to be rounded: 2^-16 of g at most).  Both have g's
+// sign and neither is 0 where g is not, 2^-24 of g at least (2^-126 for the smallest), so that the products with an infinite
+// element of X or W are two infinities of one sign, as g's own is one: with g rounded to nearest and the signed rest, 0 or the
+// other sign met the infinity and gave NaN.
+__device__ __forceinline__ float two_parts(float g, float &rest)
+{
+    const float lead = g == g ? __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, g) & 0xffff0000u) : g;
+    const float size = fabsf(lead);
+    const float left = size < INFINITY ? fmaxf(fabsf(g - lead), 0x1p-24f * size) : 0.0f;
+    rest = g == 0.0f ? 0.0f : copysignf(fmaxf(left, 0x1p-126f), g);
+    return lead;
+}
+
 // A wavefront owns 64 chunks of 16 bytes of columns and every fourth row of a tile of rows of one expert.  One pass:
 // reads dout, pre and mul, writes g and dmul, and adds g up for the bias in f32 before it is rounded, over the tile.
 template <typename T_>
@@ -78,16 +91,14 @@ __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout,
             for (int x = 0; x < N; ++x)
                 sum[x] += g[x];
             if (g_out) {
-                const u32x4 rounded = Chunk<T_>::narrow(g);
-                *reinterpret_cast<u32x4 *>(g_out + row * ldk + c) = rounded;
                 if (lo > 0) {
-                    float h[N];
-                    Chunk<T_>::widen(rounded, h);
+                    float rest[N];
 #pragma unroll
                     for (int x = 0; x < N; ++x)
-                        g[x] = fabsf(h[x]) < INFINITY ? g[x] - h[x] : 0.0f;
-                    *reinterpret_cast<u32x4 *>(g_out + row * ldk + lo + c) = Chunk<T_>::narrow(g);
+                        g[x] = two_parts(g[x], rest[x]);
+                    *reinterpret_cast<u32x4 *>(g_out + row * ldk + lo + c) = Chunk<T_>::narrow(rest);
                 }
+                *reinterpret_cast<u32x4 *>(g_out + row * ldk + c) = Chunk<T_>::narrow(g);
             }
         }
     } else if (g_out && c < lo) {   // to whole slabs

@@ -45,3 +45,37 @@ def test_nan_passes_every_activation(gpu_device, T, d_in, d_out, E, act, dtype):
         assert int(t.isnan().sum()) == n, name
         keep = ~t.isnan()
         assert torch.equal(t[keep], clean[name][keep]), name
+
+
+def _kind(t):
+    """0: finite, 1 and -1: the infinities, 2: NaN."""
+    return torch.where(t.isnan(), 2.0, torch.where(t.isinf(), t.sign(), torch.zeros_like(t))).to(torch.int8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "none"])
+@pytest.mark.parametrize("T,d_in,d_out,E", SIZES + [(1, 64, 72, 0), (4, 1000, 4096, 0), (2048, 72, 8, 0), (250, 1032, 64, 9)])
+def test_infinities_in_gradients(gpu_device, T, d_in, d_out, E, act, dtype):
+    """Infinite elements of W, X and dout, one or two of either sign in a sum, meet g whatever parts it is kept in; with act
+    none the powers of 2 in mul leave g a bf16 number, whose second part would be 0."""
+    for seed, where in enumerate(("W", "X", "dout", "all")):
+        p = _make(T, d_in, d_out, dtype, E=E, seed=seed)
+        pre, dout = _saved(p, dtype)
+        p["mul"] = torch.exp2(torch.randint(-3, 3, dout.shape, device="cuda").float()).to(dout.dtype)
+        row = T - 1
+        e = _at(T, p["offsets"], row)
+        W = p["W"][e] if E else p["W"]
+        if where in ("W", "all"):
+            W[5, 7], W[1, 9], W[6, 9] = math.inf, -math.inf, math.inf
+        if where in ("X", "all"):
+            p["X"][row, 11] = -math.inf
+            p["X"][max(0, T - 3), 3] = p["X"][row, 3] = math.inf
+        if where in ("dout", "all"):
+            dout[row, 2] = -math.inf
+        got = _backward(p, act, pre, dtype, names=("dX", "dW", "dbias"), dout=dout)
+        want = ref.linear_grad(dout, p["X"], p["W"], p["offsets"], act, pre, p["mul"])
+        for name, t in got.items():
+            value = want[name][0].reshape(t.shape)
+            if (name, where) in (("dX", "W"), ("dW", "X")) or where in ("dout", "all"):
+                assert not bool(value.isfinite().all()), "the case has an infinity"
+            assert torch.equal(_kind(t.double()), _kind(value)), f"{name}, {where}"
