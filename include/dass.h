@@ -433,9 +433,9 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  * each where its pointer is not NULL (the gradient of residual is dout).  An
  * expert without rows gets zeros in dW and dbias; rows of no expert are left as
  * they were in dX and dmul.  pre may be NULL if act is DASS_ACT_NONE and
- * dmul is not asked for.  Outputs must not overlap inputs.  g is rounded to dt for the two products (in bf16, where
- * it has up to 16384 elements or dX up to 8192, to two numbers each), and dbias
- * is summed before that; everything else is f32 and rounded once.  Sums have a fixed order: the same
+ * dmul is not asked for.  Outputs must not overlap inputs.  g is rounded to dt for the two products, and dbias
+ * is summed before that; everything else is f32 and rounded once.  (In bf16 g is two numbers, 16 bits of it and more, for both products
+ * where it has up to 16384 elements or dX up to 8192, and for dW where that has up to 8192 of all experts.)  Sums have a fixed order: the same
  * call gives the same bits on every run (with other gradients asked for, k may be split otherwise).
  *   workspace  dass_linear_backward_workspace_bytes() bytes, 16-byte aligned: g
  *            and partial sums.  A call without activation and mul, or of fewer

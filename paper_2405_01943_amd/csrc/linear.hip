@@ -5,9 +5,10 @@
 // Gradients, with g = dout * mul * act'(pre):  dX = g W,  dW = g^T X over an expert's rows,  db = sum of its g,
 // dmul = dout * act(pre).  g is read by both products, so it is written once, in dtype dt: rounded to bf16
 // there because the matrix cores take nothing wider (each term of a sum is off by half a step of its own, which adds about as
-// much to a sum as its own rounding does: 0.0023 of the whole where f32 would leave 0.0017).  Where g or dX is small
-// chance makes it more (two rows of 144: 0.0026), and there g is kept as two bf16 numbers, its leading bits and what they leave,
-// and the products run over both.  Without activation and mul, g is dout itself and nothing is written.
+// much to a sum as its own rounding does: 0.00235 of the whole where f32 would leave 0.00166).  Where g, dX or dW is small
+// chance makes it more (two rows of 144: 0.0026; dW of 8 x 8: 0.0034), and there g is kept as two bf16 numbers, its leading bits and what
+// they leave, and the products run over both.  Everywhere that would cost as much as the products do: 6001 rows over 8 experts of 4096 x
+// 11008 in one part 1174 us, in two 2140.  Without activation and mul, g is dout itself and nothing is written.
 #include "linear.h"
 
 #include <algorithm>
@@ -39,7 +40,8 @@ template <typename T_>
 __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout, int64_t ldg, const T_ *__restrict__ pre,
                                                     int64_t ldp, const T_ *__restrict__ mul, int64_t ldm, int act, int64_t cols,
                                                     Segments seg, int tile_rows, T_ *__restrict__ g_out, int64_t ldk, int64_t lo,
-                                                    T_ *__restrict__ dmul, int64_t lddm, float *__restrict__ partial, uint32_t strips)
+                                                    T_ *__restrict__ w_out, int64_t w_lo, T_ *__restrict__ dmul, int64_t lddm,
+                                                    float *__restrict__ partial, uint32_t strips)
 {
     constexpr int N = Chunk<T_>::N;
     constexpr bool FAST = sizeof(T_) == 2;
@@ -90,18 +92,19 @@ __global__ __launch_bounds__(256) void slope_kernel(const T_ *__restrict__ dout,
 #pragma unroll
             for (int x = 0; x < N; ++x)
                 sum[x] += g[x];
-            if (g_out) {
-                if (lo > 0) {
-                    float rest[N];
-#pragma unroll
-                    for (int x = 0; x < N; ++x)
-                        g[x] = two_parts(g[x], rest[x]);
-                    *reinterpret_cast<u32x4 *>(g_out + row * ldk + lo + c) = Chunk<T_>::narrow(rest);
-                }
+            if (g_out && lo == 0)
                 *reinterpret_cast<u32x4 *>(g_out + row * ldk + c) = Chunk<T_>::narrow(g);
+            if (lo > 0 || w_lo > 0) {
+                float rest[N];
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    g[x] = two_parts(g[x], rest[x]);
+                T_ *const to = lo > 0 ? g_out + row * ldk + c : w_out + row * cols + c;
+                *reinterpret_cast<u32x4 *>(to) = Chunk<T_>::narrow(g);
+                *reinterpret_cast<u32x4 *>(to + (lo > 0 ? lo : w_lo)) = Chunk<T_>::narrow(rest);
             }
         }
-    } else if (g_out && c < lo) {   // to whole slabs
+    } else if (c < lo) {   // to whole slabs
         for (int64_t row = r.lo + wave; row < end; row += 4)
             *reinterpret_cast<u32x4 *>(g_out + row * ldk + c) = *reinterpret_cast<u32x4 *>(g_out + row * ldk + lo + c) = u32x4{0, 0, 0, 0};
     }
@@ -145,24 +148,32 @@ static int sum_tile_rows(int64_t rows, int64_t cols, int dt)
     return (int)(t < (1 << 24) ? t : 1 << 24);
 }
 
-// Elements from a row's g to the second part of it, whole slabs; 0: g is in one part.  In two where it has up to 16384 elements, or dX
-// up to 8192: of more the mean squares of the errors are within a quarter of their expectation (30000 gradients of random
-// sizes: off by at most 1.5 times what the result's rounding alone is, in one part up to 1.63 times with two rows of dX).
-static int64_t second_part(int64_t rows, int64_t d_in, int64_t d_out, int dt)
-{
-    return dt == DASS_BF16 && (rows * d_out <= 16384 || rows * d_in <= 8192) ? round_up((size_t)d_out, 64) : 0;
-}
+// How g is kept, in elements.  In two parts (two_parts) where the result or g itself has so few elements that the mean squares of
+// the errors are not near their expectation: both in each row, whole slabs, for both products where g has up to 16384 elements or
+// dX up to 8192, and for dW alone, in two matrices of its own, where it has up to 8192 (of all experts).  61104 gradients of random sizes, 1 to
+// 65536 rows, widths of 8 to 4096, dense and by 2 to 33 experts: the error is 1.36 times that of a g in f32 in the mean where g is in one part,
+// 1.473 times at most, and 1.001 times at most in two; without the rule for dW 2.07.  It costs 4096 rows of 64 x 64 18.8 -> 23.2 us,
+// 65536 of 64 x 128 88 -> 138, 2^20 of 8 x 8 1160 -> 2040 and three times the g in the workspace.
+struct KeptG {
+    int64_t ld, lo;         // its rows; lo > 0: from a row's first part to the second
+    int64_t w_lo;           // > 0: dW's own two matrices follow, this far apart
+    size_t before, bytes;   // bytes of the first matrix and of all
+};
 
-// Elements of a row of the g that is kept.
-static int64_t kept_row(int64_t rows, int64_t d_in, int64_t d_out, int dt)
+static KeptG kept_g(int64_t rows, int64_t d_in, int64_t d_out, int64_t n_experts, dass_dtype dt, bool dX, bool dW)
 {
-    const int64_t lo = second_part(rows, d_in, d_out, dt);
-    return lo > 0 ? 2 * lo : d_out;
-}
-
-static size_t kept_bytes(int64_t rows, int64_t d_in, int64_t d_out, dass_dtype dt)
-{
-    return round_up((size_t)rows * (size_t)kept_row(rows, d_in, d_out, dt) * elem_bytes(dt), 256);
+    const size_t matrix = round_up((size_t)rows * (size_t)d_out * elem_bytes(dt), 256);
+    KeptG k = {d_out, 0, 0, matrix, matrix};
+    if (dt == DASS_BF16 && (rows * d_out <= 16384 || rows * d_in <= 8192)) {
+        k.lo = round_up((size_t)d_out, 64);
+        k.ld = 2 * k.lo;
+        k.before = k.bytes = round_up((size_t)rows * (size_t)k.ld * 2, 256);
+    } else if (dt == DASS_BF16 && dW && n_experts * d_out * d_in <= 8192) {
+        k.w_lo = matrix / 2;
+        k.before = dX ? matrix : 0;
+        k.bytes = k.before + 2 * matrix;
+    }
+    return k;
 }
 
 static size_t partial_bytes(int64_t rows, int64_t d_out, int64_t n_experts, int dt)
@@ -365,9 +376,10 @@ static double makespan(int64_t n1, double t1, int64_t n2, double t2, int64_t slo
 // 2056 159, 113 with 256 x 256; 8192 over 8 experts of 4096 x 14336 2000, 1863; but 512 of 1024 x 4096 34.0, 43.1, and 16384
 // of 512 x 512 57.5, 170.8, where k has to be split.  Over 97 sizes the choice is 1 % slower than the best in the mean, and 1.26
 // times as fast as two launches always.
-static int pair_of(const Plan &x, const Plan &w, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts, int parts)
+static int pair_of(const Plan &x, const Plan &w, int64_t T, int64_t d_in, int64_t d_out, int64_t n_experts, int parts_x,
+                   int parts_w)
 {
-    const int64_t slabs_x = parts * pieces(d_out, 64), slabs_w = parts * pieces(pieces(T, n_experts), 64);
+    const int64_t slabs_x = parts_x * pieces(d_out, 64), slabs_w = parts_w * pieces(pieces(T, n_experts), 64);
     const double memory = 6 + 2.0 / 5.2e6 * std::min(n_experts, T) * d_in * d_out + 2.0 / 3.38e6 * ((double)T + n_experts * d_out) * d_in;
     int best = -1;
     double best_time = x.us + w.us + 2;   // 2: the second launch
@@ -401,6 +413,7 @@ static size_t split_bytes(const Plan &plan, Product product, int64_t T, int64_t 
 
 // What a gradient's call takes and needs: g if it is kept, then the most of the bias sums and of the split products' shares.
 struct GradPlan {
+    KeptG g;    // all 0: it is not kept
     Plan x, w;
     int pair;   // the tile of both products in one launch; -1: none
     size_t bytes;
@@ -409,21 +422,23 @@ struct GradPlan {
 static GradPlan plan_grad(int64_t T, int64_t d_in, int64_t d_out, dass_dtype dt, int64_t n_experts, bool keeps_g, bool dX, bool dW,
                           bool dbias)
 {
-    const int parts = keeps_g && second_part(T, d_in, d_out, dt) > 0 ? 2 : 1;
     GradPlan p = {};
+    if (keeps_g)
+        p.g = kept_g(T, d_in, d_out, n_experts, dt, dX, dW);
+    const int parts_x = p.g.lo > 0 ? 2 : 1, parts_w = p.g.lo > 0 || p.g.w_lo > 0 ? 2 : 1;
     p.pair = -1;
     if (dX)
-        p.x = plan_of(kInputGrad, dt, T, d_in, d_out, n_experts, parts);
+        p.x = plan_of(kInputGrad, dt, T, d_in, d_out, n_experts, parts_x);
     if (dW)
-        p.w = plan_of(kWeightGrad, dt, T, d_in, d_out, n_experts, parts);
+        p.w = plan_of(kWeightGrad, dt, T, d_in, d_out, n_experts, parts_w);
     if (dX && dW && dt == DASS_BF16)
-        p.pair = pair_of(p.x, p.w, T, d_in, d_out, n_experts, parts);
+        p.pair = pair_of(p.x, p.w, T, d_in, d_out, n_experts, parts_x, parts_w);
     p.bytes = dbias ? partial_bytes(T, d_out, n_experts, dt) : 0;
     if (dX && p.pair < 0)
         p.bytes = std::max(p.bytes, split_bytes(p.x, kInputGrad, T, d_in, d_out, n_experts));
     if (dW && p.pair < 0)
         p.bytes = std::max(p.bytes, split_bytes(p.w, kWeightGrad, T, d_in, d_out, n_experts));
-    p.bytes += keeps_g ? kept_bytes(T, d_in, d_out, dt) : 0;
+    p.bytes += p.g.bytes;
     return p;
 }
 
@@ -464,35 +479,33 @@ static dass_status run_linear_grad(const char *fn, const dass_linear_grad_task &
     constexpr int N = Chunk<T_>::N;
     const Segments seg = {t.offsets, t.T, (int)t.n_experts};
     const bool own_g = keeps_g(t);
-    const int64_t lo = own_g ? second_part(t.T, t.d_in, t.d_out, t.dt) : 0, ldk = kept_row(t.T, t.d_in, t.d_out, t.dt);
-    const T_ *g = static_cast<const T_ *>(t.dout);
-    int64_t ldg = t.ldg;
     // the workspace: g if it is kept, then the partial sums of the bias, whose place the split products take after them
-    char *const shares = workspace + (own_g ? kept_bytes(t.T, t.d_in, t.d_out, t.dt) : 0);
+    char *const shares = workspace + plan.g.bytes;
+    T_ *const kept = plan.g.before > 0 ? reinterpret_cast<T_ *>(workspace) : nullptr;
+    T_ *const kept_w = plan.g.w_lo > 0 ? reinterpret_cast<T_ *>(workspace + plan.g.before) : nullptr;
     const BiasSums bias = {reinterpret_cast<float *>(shares), t.d_out, seg, sum_tile_rows(t.T, t.d_out, t.dt), t.dbias};
     if (own_g || t.dbias || t.dmul) {
-        T_ *kept = own_g ? reinterpret_cast<T_ *>(workspace) : nullptr;
         const int64_t numbers = tile_numbers(seg, bias.tile_rows), strips = (t.d_out + 64 * N - 1) / (64 * N);
         if (numbers > 0xffffffffLL / 256 / strips)
             return fail(DASS_ERR_SHAPE, "%s: too many tiles for one launch; split the rows", fn);
         hipLaunchKernelGGL(slope_kernel<T_>, dim3((unsigned)(numbers * strips)), dim3(256), 0, stream,
                            static_cast<const T_ *>(t.dout), t.ldg, static_cast<const T_ *>(t.pre), t.ldp,
-                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, bias.tile_rows, kept, ldk, lo,
-                           static_cast<T_ *>(t.dmul), t.lddm, t.dbias ? reinterpret_cast<float *>(shares) : nullptr, (uint32_t)strips);
+                           static_cast<const T_ *>(t.mul), t.ldm, (int)t.act, t.d_out, seg, bias.tile_rows, kept, plan.g.ld, plan.g.lo,
+                           kept_w, plan.g.w_lo, static_cast<T_ *>(t.dmul), t.lddm,
+                           t.dbias ? reinterpret_cast<float *>(shares) : nullptr, (uint32_t)strips);
         const dass_status s = check_launch("slope kernel");
         if (s != DASS_OK)
             return s;
-        if (own_g) {
-            g = kept;
-            ldg = ldk;
-        }
     }
 
     Operands<T_> ax = {}, aw = {};
     Epilogue<T_> ex = {}, ew = {};
-    ax.P = aw.P = g;
-    ax.ldp = aw.ldp = ldg;
-    ax.lo = aw.lo = lo;
+    ax.P = own_g ? kept : static_cast<const T_ *>(t.dout);
+    ax.ldp = own_g ? plan.g.ld : t.ldg;
+    ax.lo = plan.g.lo;
+    aw.P = kept_w ? kept_w : ax.P;
+    aw.ldp = kept_w ? t.d_out : ax.ldp;
+    aw.lo = kept_w ? plan.g.w_lo : plan.g.lo;
     ax.seg = aw.seg = seg;
     ex.cols = ew.cols = t.d_in;
     ex.act = ew.act = DASS_ACT_NONE;

@@ -54,7 +54,8 @@ def _kind(t):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ["silu", "none"])
-@pytest.mark.parametrize("T,d_in,d_out,E", SIZES + [(1, 64, 72, 0), (4, 1000, 4096, 0), (2048, 72, 8, 0), (250, 1032, 64, 9)])
+@pytest.mark.parametrize("T,d_in,d_out,E", SIZES + [(1, 64, 72, 0), (4, 1000, 4096, 0), (2048, 72, 8, 0), (250, 1032, 64, 9), (4096, 16, 8, 0), (4099, 64, 72, 0),
+                                                     (5000, 16, 24, 5)])
 def test_infinities_in_gradients(gpu_device, T, d_in, d_out, E, act, dtype):
     """Infinite elements of W, X and dout, one or two of either sign in a sum, meet g whatever parts it is kept in; with act
     none the powers of 2 in mul leave g a bf16 number, whose second part would be 0."""
