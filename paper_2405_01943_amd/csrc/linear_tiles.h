@@ -84,8 +84,8 @@ __device__ __forceinline__ u32x4 raw_buffer(const void *p, int bytes)
 // by hand where one is not.  Beside the builtin the compiler waits for every such load before each transposing LDS read (it takes the
 // read to depend on them), which empties the pipeline once a load: dX and dW of 6000 rows of 4096 x 11008 1590 us, by
 // hand 548 and 444; of products without such reads the builtin is 4 % ahead.  (Not a template: with arguments that depend on
-// one, the host pass rejects the builtin.)  The block by hand writes no register but m0; the waits for it are
-// those before the barriers.  Its s_nop covers the wait states between a scalar register's last write and its use as an address.
+// one, the host pass rejects the builtin.)  The block by hand writes no register; m0 is an operand of it, so that
+// the compiler knows what it holds.  The waits for it are those before the barriers.  Its s_nop covers the wait states between a scalar register's last write and its use as an address.
 __device__ __forceinline__ void load_to_lds(const u32x4 &buffer, char *dst, uint32_t lane_off, int off)
 {
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
@@ -95,8 +95,7 @@ __device__ __forceinline__ void load_to_lds(const u32x4 &buffer, char *dst, uint
 __device__ __forceinline__ void load_to_lds_by_hand(const u32x4 &buffer, char *dst, uint32_t lane_off, int off)
 {
     const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr_t)dst;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(lane_off), "s"(buffer),
-                 "s"(off) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(at), "v"(lane_off), "s"(buffer), "s"(off) : "memory");
 }
 
 __device__ __forceinline__ void block_barrier()
