@@ -377,7 +377,8 @@ dass_status dass_down_proj_sparse24(const void *Y, int64_t T, int64_t ldy, const
  *   residual is dout.
  *
  * X, out of the gather etc. are rows of d elements of dtype dt; d is a multiple
- * of 8 (bf16) or 4 (f32) up to 2^24.  Entries of place outside 0 .. T k - 1 count as
+ * of 8 (bf16) or 4 (f32) up to 2^24; rows lie at most 2^36 elements apart, and rows times their stride are at most 2^46.
+ * Entries of place outside 0 .. T k - 1 count as
  * pairs that go nowhere.  place must not hold a row twice where rows are written.
  * Outputs must not overlap inputs, but for the residual (with its stride).
  */
@@ -423,7 +424,7 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  * All of dtype dt (bf16 or f32); sums and epilogue are f32, rounded once (pre
  * and out each).  d_in and d_out are multiples of 8 (bf16) or 4 (f32) up to 2^20, T is
  * at most 2^30.  Rows of X and W, and of dout below, lie less than 8 MiB apart, others at most
- * 2^36 elements.
+ * 2^36 elements, and rows times their stride are at most 2^46 elements.
  *
  * dass_linear_backward gives, with g = dout * mul * act'(pre),
  *

@@ -33,6 +33,10 @@ inline bool valid_axis(int a) { return a == DASS_AXIS_ROWS || a == DASS_AXIS_COL
 inline int elem_bytes(int dt) { return dt == DASS_BF16 ? 2 : 4; }
 inline int vec_elems(int dt) { return 16 / elem_bytes(dt); }  // elements per 16-byte access
 
+// Rows times their stride that the linear layers and the experts' rows take, in elements: 2^48 bytes of f32, all that an address
+// reaches here, so that no product of a row and a stride leaves 64 bits.
+constexpr int64_t kMaxSpan = 1LL << 46;
+
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Turn a failed launch into DASS_ERR_HIP with the runtime's message.

@@ -321,12 +321,15 @@ static dass_status check_pairs(const char *fn, int64_t T, int64_t k)
 }
 
 // A matrix of rows of d elements: pointer and stride.
-static dass_status check_rows(const char *fn, const char *name, const void *p, int64_t ld, int64_t d, int vec)
+static dass_status check_rows(const char *fn, const char *name, const void *p, int64_t rows, int64_t ld, int64_t d, int vec)
 {
     if (!p)
         return fail(DASS_ERR_NULL, "%s: %s must not be NULL", fn, name);
     if (ld < d || ld > 1LL << 36)
         return fail(DASS_ERR_SHAPE, "%s: rows of %s: stride %lld < d=%lld or beyond 2^36", fn, name, (long long)ld, (long long)d);
+    if (rows > kMaxSpan / ld)
+        return fail(DASS_ERR_SHAPE, "%s: %lld rows of %s with stride %lld span more than 2^46 elements", fn, (long long)rows, name,
+                    (long long)ld);
     if (!aligned16(p) || ld % vec != 0)
         return fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
     return DASS_OK;
@@ -404,9 +407,9 @@ extern "C" dass_status dass_expert_gather(const void *X, int64_t T, int64_t ldx,
     if (s == DASS_OK)
         s = check_pairs(fn, T, k);
     if (s == DASS_OK)
-        s = check_rows(fn, "X", X, ldx, d, vec_elems(dt));
+        s = check_rows(fn, "X", X, T, ldx, d, vec_elems(dt));
     if (s == DASS_OK)
-        s = check_rows(fn, "out", out, ldo, d, vec_elems(dt));
+        s = check_rows(fn, "out", out, T * k, ldo, d, vec_elems(dt));
     if (s != DASS_OK)
         return s;
     if (!place)
@@ -436,11 +439,11 @@ extern "C" dass_status dass_expert_combine(const void *Y, int64_t ldy, const int
     if (s == DASS_OK)
         s = check_pairs(fn, T, k);
     if (s == DASS_OK)
-        s = check_rows(fn, "Y", Y, ldy, d, vec_elems(dt));
+        s = check_rows(fn, "Y", Y, T * k, ldy, d, vec_elems(dt));
     if (s == DASS_OK && residual)
-        s = check_rows(fn, "residual", residual, ldr, d, vec_elems(dt));
+        s = check_rows(fn, "residual", residual, T, ldr, d, vec_elems(dt));
     if (s == DASS_OK)
-        s = check_rows(fn, "out", out, ldo, d, vec_elems(dt));
+        s = check_rows(fn, "out", out, T, ldo, d, vec_elems(dt));
     if (s != DASS_OK)
         return s;
     if (!place)
@@ -479,11 +482,11 @@ extern "C" dass_status dass_expert_combine_backward(const void *dout, int64_t ld
     if (s == DASS_OK)
         s = check_pairs(fn, T, k);
     if (s == DASS_OK)
-        s = check_rows(fn, "dout", dout, ldg, d, vec_elems(dt));
+        s = check_rows(fn, "dout", dout, T, ldg, d, vec_elems(dt));
     if (s == DASS_OK)
-        s = check_rows(fn, "Y", Y, ldy, d, vec_elems(dt));
+        s = check_rows(fn, "Y", Y, T * k, ldy, d, vec_elems(dt));
     if (s == DASS_OK)
-        s = check_rows(fn, "dY", dY, lddy, d, vec_elems(dt));
+        s = check_rows(fn, "dY", dY, T * k, lddy, d, vec_elems(dt));
     if (s != DASS_OK)
         return s;
     if (!place || !weights || !dweights)

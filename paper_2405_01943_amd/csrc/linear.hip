@@ -17,7 +17,7 @@
 namespace dass {
 
 constexpr int kMaxLinearExperts = 1024;
-constexpr int64_t kMaxRows = 1 << 30, kMaxWidth = 1 << 20, kMaxStride = 1LL << 36;   // products of sizes stay within 64 bits
+constexpr int64_t kMaxRows = 1 << 30, kMaxWidth = 1 << 20, kMaxStride = 1LL << 36;
 constexpr int64_t kMaxReadRow = 1 << 23;   // bytes between rows that a tile addresses: 256 of them with 32-bit offsets
 
 // ------------------------------------------------------ element-wise gradient and sums --
@@ -189,8 +189,8 @@ struct Arguments {
     int vec;
     dass_status status = DASS_OK;
 
-    // a matrix of rows of `width` elements; absent optional ones are fine
-    void matrix(const char *name, const void *p, int64_t ld, int64_t width, bool required, int64_t longest = kMaxStride)
+    // a matrix of `rows` rows of `width` elements; absent optional ones are fine
+    void matrix(const char *name, const void *p, int64_t rows, int64_t ld, int64_t width, bool required, int64_t longest = kMaxStride)
     {
         if (status != DASS_OK || (!p && !required))
             return;
@@ -199,6 +199,9 @@ struct Arguments {
         else if (ld < width || ld > longest)
             status = fail(DASS_ERR_SHAPE, "%s: row stride %lld of %s is shorter than its rows of %lld or beyond %lld", fn, (long long)ld,
                           name, (long long)width, (long long)longest);
+        else if (rows > kMaxSpan / ld)
+            status = fail(DASS_ERR_SHAPE, "%s: %lld rows of %s with stride %lld span more than 2^46 elements", fn, (long long)rows, name,
+                          (long long)ld);
         else if (!aligned16(p) || ld % vec != 0)
             status = fail(DASS_ERR_ALIGN, "%s: %s must be 16-byte aligned, its row stride a multiple of %d elements", fn, name, vec);
     }
@@ -574,12 +577,12 @@ extern "C" dass_status dass_linear(const dass_linear_task *task, void *workspace
     Arguments c{fn, valid_dtype(t.dt) ? vec_elems(t.dt) : 1};
     c.sizes(t.T, t.d_in, t.d_out, t.n_experts, t.offsets, (int)t.dt, (int)t.act);
     const int64_t read = longest_read(t.dt);
-    c.matrix("X", t.X, t.ldx, t.d_in, true, read);
-    c.matrix("W", t.W, t.ldw, t.d_in, true, read);
-    c.matrix("mul", t.mul, t.ldm, t.d_out, false);
-    c.matrix("residual", t.residual, t.ldr, t.d_out, false);
-    c.matrix("pre_out", t.pre_out, t.ldp, t.d_out, false);
-    c.matrix("out", t.out, t.ldo, t.d_out, true);
+    c.matrix("X", t.X, t.T, t.ldx, t.d_in, true, read);
+    c.matrix("W", t.W, t.d_out, t.ldw, t.d_in, true, read);
+    c.matrix("mul", t.mul, t.T, t.ldm, t.d_out, false);
+    c.matrix("residual", t.residual, t.T, t.ldr, t.d_out, false);
+    c.matrix("pre_out", t.pre_out, t.T, t.ldp, t.d_out, false);
+    c.matrix("out", t.out, t.T, t.ldo, t.d_out, true);
     c.vector("bias", t.bias);
     c.stride("W", t.expert_stride, t.ldw, t.d_in, t.d_out, t.n_experts);
     c.apart("out", t.out, {t.X, t.W, t.bias, t.pre_out});
@@ -630,14 +633,14 @@ extern "C" dass_status dass_linear_backward(const dass_linear_grad_task *task, v
     if (t.dmul && !t.mul)
         return fail(DASS_ERR_NULL, "%s: dmul without mul", fn);
     const int64_t read = longest_read(t.dt);
-    c.matrix("dout", t.dout, t.ldg, t.d_out, true, read);
-    c.matrix("X", t.X, t.ldx, t.d_in, t.dW != nullptr, read);
-    c.matrix("W", t.W, t.ldw, t.d_in, t.dX != nullptr, read);
-    c.matrix("pre", t.pre, t.ldp, t.d_out, t.act != DASS_ACT_NONE || t.dmul);
-    c.matrix("mul", t.mul, t.ldm, t.d_out, false);
-    c.matrix("dX", t.dX, t.lddx, t.d_in, false);
-    c.matrix("dW", t.dW, t.lddw, t.d_in, false);
-    c.matrix("dmul", t.dmul, t.lddm, t.d_out, false);
+    c.matrix("dout", t.dout, t.T, t.ldg, t.d_out, true, read);
+    c.matrix("X", t.X, t.T, t.ldx, t.d_in, t.dW != nullptr, read);
+    c.matrix("W", t.W, t.d_out, t.ldw, t.d_in, t.dX != nullptr, read);
+    c.matrix("pre", t.pre, t.T, t.ldp, t.d_out, t.act != DASS_ACT_NONE || t.dmul);
+    c.matrix("mul", t.mul, t.T, t.ldm, t.d_out, false);
+    c.matrix("dX", t.dX, t.T, t.lddx, t.d_in, false);
+    c.matrix("dW", t.dW, t.d_out, t.lddw, t.d_in, false);
+    c.matrix("dmul", t.dmul, t.T, t.lddm, t.d_out, false);
     c.vector("dbias", t.dbias);
     const void *const inputs[] = {t.dout, t.X, t.W, t.pre, t.mul};
     void *const outputs[] = {t.dX, t.dW, t.dbias, t.dmul};
