@@ -9,7 +9,8 @@
  *   - All data pointers are DEVICE pointers owned by the caller.  The library
  *     never allocates, frees or synchronises.  Work is enqueued on
  *     `hip_stream` (a hipStream_t passed as void*; NULL = the default stream)
- *     and calls are ordered by that stream.
+ *     and calls are ordered by that stream.  The current device is the one of
+ *     the stream and the buffers.
  *   - Matrices are row-major in the paper's transposed layout (Sec. 3):
  *     Gate-Proj and Up-Proj are [d_int, d_hidden], Down-Proj is
  *     [d_hidden, d_int]; `ld*` is the row stride in elements.
@@ -17,7 +18,8 @@
  *     8 elements (bf16) or 4 elements (f32); otherwise DASS_ERR_ALIGN.
  *   - All argument checks happen on the host before the first HIP call, so a
  *     rejected call has touched nothing.
- *   - Inputs must be finite.  The result for NaN or Inf inputs is undefined.
+ *   - Inputs must be finite.  The result for NaN or Inf inputs is undefined,
+ *     except where a call says more (dass_expert_*, dass_linear*).
  *   - Thread safe; the only library state is a thread-local error string
  *     (and, for dass_score_mask_unstructured_static, one device array).
  *     Calls enqueued on different streams may run at the same time as long
@@ -381,6 +383,7 @@ dass_status dass_down_proj_sparse24(const void *Y, int64_t T, int64_t ldy, const
  * Entries of place outside 0 .. T k - 1 count as
  * pairs that go nowhere.  place must not hold a row twice where rows are written.
  * Outputs must not overlap inputs, but for the residual (with its stride).
+ * NaN and infinities are copied, and added up as f32 does.
  */
 size_t dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t n_experts);
 
@@ -438,6 +441,7 @@ dass_status dass_expert_combine_backward(const void *dout, int64_t ldg, const vo
  * is summed before that; everything else is f32 and rounded once.  (In bf16 g is two numbers, 16 bits of it and more, for both products
  * where it has up to 16384 elements or dX up to 8192, and for dW where that has up to 8192 of all experts.)  Sums have a fixed order: the same
  * call gives the same bits on every run (with other gradients asked for, k may be split otherwise).
+ * NaN and infinities give what the formulas give, in the rows and experts that hold them: a NaN passes every activation and slope.
  *   workspace  dass_linear_backward_workspace_bytes() bytes, 16-byte aligned: g
  *            and partial sums.  A call without activation and mul, or of fewer
  *            gradients, needs less and takes less.

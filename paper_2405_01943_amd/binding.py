@@ -482,7 +482,7 @@ _NEEDS_WORKSPACE = 6     # DASS_ERR_WORKSPACE
 
 
 def _on_device(stream, *tensors) -> int:
-    """The handle of the stream that a call goes to; every tensor must be on that stream's GPU."""
+    """The handle of the stream that a call goes to; every tensor must be on its GPU, and that the current one."""
     device = None
     for t in tensors:
         if t is not None:
@@ -491,9 +491,11 @@ def _on_device(stream, *tensors) -> int:
                 if device is not None or where < 0:
                     raise ValueError("every tensor must be on the GPU" if where < 0 else f"tensors on GPUs {device} and {where}")
                 device = where
-    current = torch.cuda.current_device() if stream is None else stream.device_index
-    if current != device:
-        raise ValueError(f"the tensors are on GPU {device}, the stream is of GPU {current}")
+    current = torch.cuda.current_device()
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"the tensors are on GPU {device}, the stream is of GPU {stream.device_index}")
+    if current != device:       # the library's launches reserve LDS on the current GPU
+        raise ValueError(f"the tensors are on GPU {device}, the current one is GPU {current}")
     return _raw_stream(current) if stream is None and _raw_stream is not None else _stream(stream)
 
 
