@@ -209,7 +209,8 @@ def _scratch(nbytes: int, device, stream=None) -> torch.Tensor:
     released when the call returns, so it is taken from the blocks of the stream the kernels run
     on: one of another stream's could still be in use by the kernels queued there.  A caller
     that wants no allocation on its path passes ``workspace`` itself."""
-    if stream is None:
+    # (the current stream given by name takes its blocks as they come: 7.3 us through the context, 1.5 without)
+    if stream is None or (_raw_stream is not None and stream.cuda_stream == _raw_stream(stream.device_index)):
         return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2405_01943_amd as dass
+from paper_2405_01943_amd import binding
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +93,18 @@ def test_a_stream_of_another_gpu_is_refused(gpu_device, monkeypatch):
                  lambda: dass.linear_backward(c.y, c.rows, c.W, dX=c.dr, offsets=c.offsets, stream=mine)):
         with pytest.raises(ValueError, match="current"):
             call()
+
+
+def test_a_workspace_of_the_current_stream_is_not_switched_to(gpu_device, monkeypatch):
+    """The current stream given by name: its blocks come without entering it again; another stream's do not."""
+    device = torch.device("cuda", torch.cuda.current_device())
+    current, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    entered = []
+    switch = torch.cuda.stream
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: entered.append(s) or switch(s))
+    at = binding._scratch(5 << 20, device).data_ptr()
+    assert binding._scratch(5 << 20, device, current).data_ptr() == at and not entered
+    assert binding._scratch(5 << 20, device, side).data_ptr() != at and entered == [side]
+    with switch(side):
+        assert binding._scratch(5 << 20, device, side).data_ptr() != at and entered == [side]
+        assert binding._scratch(5 << 20, device, current).data_ptr() == at and entered == [side, current]
