@@ -200,7 +200,10 @@ static dass_status launch_rows(const char *fn, const Operands<T_> &a, const Epil
 
 // Wavefronts of a workgroup and loads that each has on its way, in graphs: one row of 4096 x 11008 4 wavefronts x 8 fragments 20.0
 // us, 8 x 4 19.1, 16 x 4 17.7; of 4096 x 4096 9.4, 8.8, 8.3; but of 1024 x 4096 4.0 (x 4 3.9), 4.0, 5.1, four rows of 512 x 512
-// 3.4 (x 4 2.8), 3.4, 3.6.
+// 3.4 (x 4 2.8), 3.4, 3.6.  At the limit, 4 and 16 wavefronts on weights that no cache holds: one row to 14336 columns from 1536 11.8 and
+// 13.8, 2048 15.6 and 14.0, 2560 17.9 and 18.8, 3584 22.3 and 23.4, 4096 25.0 and 23.6, 5120 31.0 and 33.1, 8192 52.2 and 45.4; 16 rows
+// over 8 experts to 4096 columns from 2048 27.8 and 30.4, 3584 42.6 and 45.4, 4096 48.4 and 44.9, 8192 101 and 89.  (16 wavefronts take
+// 2048 of k at a time, so that they lead at its multiples, and lose up to a tenth between them.)
 dass_status launch_few(const char *fn, const Plan &, const Operands<uint16_t> &a, const Epilogue<uint16_t> &ep, hipStream_t stream)
 {
     if (a.depth >= 4096)
